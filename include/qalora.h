@@ -365,6 +365,39 @@ int qalora_adamw_step(const qalora_adamw* hp, int step, int n_tensors, float* co
                       const size_t* numel, int zero_grads, float* grad_norm, void* ws,
                       size_t ws_bytes, void* stream);
 
+/* The orthogonalised update ("Muon") of a list of matrices, in place of qalora_adamw_step for
+ * the adapters (only A and B are trained, Sec. 3.1): momentum, then a matrix with the update's singular
+ * vectors and singular values near one, by Newton-Schulz products.  For each matrix [rows, cols]:
+ *   m = momentum m + g;   u = nesterov ? g + momentum m : m;
+ *   X = u / (|u|_F + eps), as [shorter side, longer side];
+ *   `steps` times:  G = X X^T,  X = a X + (b G + c G G) X;
+ *   p = p (1 - lr weight_decay) - lr scale X.
+ * (3.4445, -4.7750, 2.0315) with five steps are the published coefficients (K. Jordan, Muon, 2024): they bring singular
+ * values from 2e-3 of |u|_F on to 0.7 .. 1.2; (1.5, -0.5, 0) converges to one, but slowly.
+ * scale: 1; sqrt(max(1, rows / cols)); or 0.2 sqrt(max(rows, cols)), the mean square of an AdamW step.
+ * params, grads, momentum: HOST arrays of n_tensors DEVICE pointers (fp32, row-major, 16-byte aligned, no two the same);
+ * params and momentum are updated in place; grads are read, and set to zero afterwards if zero_grads != 0.
+ * rows, cols: HOST arrays.  The shorter side is at most QALORA_MUON_MAX_SHORT (the rank of an adapter;
+ * QALORA_EUNSUPPORTED otherwise); the longer one is any.  eps > 0; a matrix of zeros gets the update zero.
+ * A matrix with an infinity or a NaN in u becomes NaN, the others do not see it.
+ * ws: qalora_muon_workspace_bytes(n_tensors, rows, cols) bytes (0 for a list that is not acceptable), about what the matrices
+ * take themselves.  fp32 arithmetic, sums in a fixed order: a step is bit-reproducible.  Errors of the sums, about 2^-24 of
+ * |u|_F, grow with the smallest singular values, by up to a^steps.  May be captured into a HIP graph, after an eager call
+ * of as many steps. */
+#define QALORA_MUON_MAX_TENSORS 32
+#define QALORA_MUON_MAX_SHORT 128
+#define QALORA_MUON_MAX_STEPS 16
+enum qalora_muon_scale { QALORA_MUON_SCALE_NONE = 0, QALORA_MUON_SCALE_SHAPE = 1, QALORA_MUON_SCALE_RMS = 2 };
+typedef struct qalora_muon {
+  float lr, momentum, weight_decay, eps;
+  float a, b, c;
+  int32_t steps, nesterov, scale_mode;
+} qalora_muon;
+size_t qalora_muon_workspace_bytes(int n_tensors, const int32_t* rows, const int32_t* cols);
+int qalora_muon_step(const qalora_muon* hp, int n_tensors, float* const* params, float* const* grads,
+                     float* const* momentum, const int32_t* rows, const int32_t* cols, int zero_grads, void* ws,
+                     size_t ws_bytes, void* stream);
+
 /* Measurement aid (used by the benchmark, not part of the layer): arm a pair of HIP events
  * (hipEvent_t passed as void*, created by the caller with timing enabled).  The next dense
  * contraction kernel of the given direction (0 = the y = x W~ kernel of qalora_forward,

@@ -39,6 +39,7 @@ EXPORTS = (
     "qalora_shared_kept_bytes", "qalora_shared_workspace_bytes", "qalora_forward_shared",
     "qalora_quantize_compensated",
     "qalora_backward_shared", "qalora_swiglu_forward_wide", "qalora_swiglu_backward_wide",
+    "qalora_muon_workspace_bytes", "qalora_muon_step",
 )
 
 
@@ -116,6 +117,9 @@ def load() -> ctypes.CDLL:
     lib.qalora_adamw_workspace_bytes.restype = sz
     lib.qalora_adamw_workspace_bytes.argtypes = [i, vp]
     lib.qalora_adamw_step.argtypes = [vp, i, i, vp, vp, vp, vp, vp, i, vp, vp, sz, vp]
+    lib.qalora_muon_workspace_bytes.restype = sz
+    lib.qalora_muon_workspace_bytes.argtypes = [i, vp, vp]
+    lib.qalora_muon_step.argtypes = [vp, i, vp, vp, vp, vp, vp, i, vp, sz, vp]
     lib.qalora_beta_from_zero_point.argtypes = [cp, vp, vp, vp, vp]
     lib.qalora_zero_point_from_beta.argtypes = [cp, vp, vp, vp, vp]
     _lib = lib
@@ -660,6 +664,56 @@ def adamw_step(hp: AdamW, step: int, params, grads, exp_avg, exp_avg_sq, zero_gr
     rc = load().qalora_adamw_step(ctypes.byref(hp), int(step), n, ptrs[0], ptrs[1], ptrs[2], ptrs[3], numel,
                                   1 if zero_grads else 0, _p(grad_norm), _p(ws), ws.numel(), _stream())
     _check(rc, "qalora_adamw_step")
+
+
+MUON_SCALE_NONE, MUON_SCALE_SHAPE, MUON_SCALE_RMS = 0, 1, 2
+
+
+class Muon(ctypes.Structure):
+    """Mirror of ``qalora_muon``; a, b, c, steps and eps default to the published ones."""
+    _fields_ = [("lr", ctypes.c_float), ("momentum", ctypes.c_float), ("weight_decay", ctypes.c_float),
+                ("eps", ctypes.c_float), ("a", ctypes.c_float), ("b", ctypes.c_float), ("c", ctypes.c_float),
+                ("steps", ctypes.c_int32), ("nesterov", ctypes.c_int32), ("scale_mode", ctypes.c_int32)]
+
+    def __init__(self, lr=0.0, momentum=0.95, weight_decay=0.0, eps=1e-7, a=3.4445, b=-4.7750, c=2.0315, steps=5,
+                 nesterov=True, scale_mode=MUON_SCALE_RMS):
+        super().__init__(lr, momentum, weight_decay, eps, a, b, c, steps, 1 if nesterov else 0, scale_mode)
+
+
+def _sides(tensors):
+    rows, cols = (array.array("i", (int(t.shape[k]) for t in tensors)) for k in (0, 1))
+    return rows, cols
+
+
+def muon_workspace_bytes(tensors) -> int:
+    """Workspace of muon_step() over matrices of these shapes; 0 where they are not acceptable."""
+    rows, cols = _sides(tensors)
+    return int(load().qalora_muon_workspace_bytes(len(rows), rows.buffer_info()[0], cols.buffer_info()[0]))
+
+
+def muon_step(hp: Muon, params, grads, momentum, zero_grads=False, ws=None):
+    """One orthogonalised step (see qalora_muon_step) over lists of fp32 device matrices, one side of each at most
+    128; ``params`` and ``momentum`` are updated in place."""
+    n = len(params)
+    if n == 0:
+        raise ValueError("params: no tensors")
+    for ts, nm in ((params, "params"), (grads, "grads"), (momentum, "momentum")):
+        if len(ts) != n:
+            raise ValueError(f"{nm}: {len(ts)} tensors, expected {n}")
+        for t, p0 in zip(ts, params):
+            _need(t, nm, torch.float32, tuple(p0.shape), device=params[0].device)
+            if t.dim() != 2:
+                raise ValueError(f"{nm}: shape {tuple(t.shape)}, expected a matrix")
+    rows, cols = _sides(params)
+    table = array.array("Q", (t.data_ptr() for ts in (params, grads, momentum) for t in ts))
+    ptrs = [table.buffer_info()[0] + 8 * n * i for i in range(3)]
+    if ws is None:
+        ws = torch.empty(max(muon_workspace_bytes(params), 16), dtype=torch.uint8, device=params[0].device)
+    _need(ws, "ws", device=params[0].device)
+    rc = load().qalora_muon_step(ctypes.byref(hp), n, ptrs[0], ptrs[1], ptrs[2], rows.buffer_info()[0],
+                                 cols.buffer_info()[0], 1 if zero_grads else 0, _p(ws), ws.numel() * ws.element_size(),
+                                 _stream())
+    _check(rc, "qalora_muon_step")
 
 
 def profile_copy(dst: torch.Tensor, src: torch.Tensor):

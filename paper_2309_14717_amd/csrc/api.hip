@@ -1056,6 +1056,51 @@ int qalora_adamw_step(const qalora_adamw* hp, int step, int n_tensors, float* co
              : QALORA_EHIP;
 }
 
+size_t qalora_muon_workspace_bytes(int n_tensors, const int32_t* rows, const int32_t* cols) {
+  MuonTable t;
+  bool unsupported;
+  return align_up(muon_table(n_tensors, rows, cols, t, unsupported) * sizeof(float));
+}
+
+int qalora_muon_step(const qalora_muon* hp, int n_tensors, float* const* params, float* const* grads,
+                     float* const* momentum, const int32_t* rows, const int32_t* cols, int zero_grads, void* ws,
+                     size_t ws_bytes, void* stream) {
+  if (!hp || !params || !grads || !momentum) return QALORA_EINVAL;
+  if (!(hp->momentum >= 0.0f && hp->momentum < 1.0f) || !(hp->eps > 0.0f) || !(hp->lr >= 0.0f) ||
+      !(hp->weight_decay >= 0.0f) || !std::isfinite(hp->a) || !std::isfinite(hp->b) || !std::isfinite(hp->c))
+    return QALORA_EINVAL;
+  if (hp->steps < 1 || hp->steps > QALORA_MUON_MAX_STEPS) return QALORA_EINVAL;
+  if (hp->scale_mode < QALORA_MUON_SCALE_NONE || hp->scale_mode > QALORA_MUON_SCALE_RMS) return QALORA_EINVAL;
+  MuonTable t;
+  bool unsupported;
+  const size_t floats = muon_table(n_tensors, rows, cols, t, unsupported);
+  if (floats == 0) return unsupported ? QALORA_EUNSUPPORTED : QALORA_EINVAL;
+  for (int i = 0; i < n_tensors; ++i) {
+    if (!params[i] || !grads[i] || !momentum[i]) return QALORA_EINVAL;
+    if (misaligned(params[i]) || misaligned(grads[i]) || misaligned(momentum[i])) return QALORA_EALIGN;
+    t.t[i].p = params[i];
+    t.t[i].g = grads[i];
+    t.t[i].m = momentum[i];
+    const double r = rows[i], c = cols[i];
+    const double scale = hp->scale_mode == QALORA_MUON_SCALE_RMS     ? 0.2 * std::sqrt(std::max(r, c))
+                         : hp->scale_mode == QALORA_MUON_SCALE_SHAPE ? std::sqrt(std::max(1.0, r / c))
+                                                                     : 1.0;
+    t.t[i].step_size = (float)((double)hp->lr * scale);
+  }
+  if (misaligned(ws)) return QALORA_EALIGN;
+  if (!ws || ws_bytes < floats * sizeof(float)) return QALORA_EWORKSPACE;
+  MuonHyper h{};
+  h.momentum = hp->momentum;
+  h.eps = hp->eps;
+  h.a = hp->a;
+  h.b = hp->b;
+  h.c = hp->c;
+  h.decay = (float)(1.0 - (double)hp->lr * (double)hp->weight_decay);
+  h.nesterov = hp->nesterov ? 1 : 0;
+  h.zero_grads = zero_grads ? 1 : 0;
+  return launch_muon(t, h, hp->steps, static_cast<float*>(ws), as_stream(stream)) == hipSuccess ? QALORA_OK : QALORA_EHIP;
+}
+
 int qalora_profile_arm(int direction, void* start_event, void* stop_event) {
   if (direction != 0 && direction != 1) return QALORA_EINVAL;
   g_profile_hook[direction] = ProfileHook{static_cast<hipEvent_t>(start_event),

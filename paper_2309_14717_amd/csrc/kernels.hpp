@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "grads_plan.hpp"
+#include "muon_plan.hpp"
 
 namespace qalora {
 
@@ -293,6 +294,15 @@ struct OptHyper {
   int zero_grads;
 };
 hipError_t launch_adamw(const OptTensors& t, const OptHyper& h, float* partial, float* norm_out, hipStream_t st);
+
+// --- muon.hip: the orthogonalised update of up to 32 matrices ------------------------------
+struct MuonHyper {
+  float momentum, eps;
+  float a, b, c;  // of the polynomial a t + b t^3 + c t^5
+  float decay;    // 1 - lr * weight_decay
+  int nesterov, zero_grads;
+};
+hipError_t launch_muon(const MuonTable& t, const MuonHyper& h, int steps, float* ws, hipStream_t st);
 
 // --- probe.hip (measurement aid): issue-rate probe of the matrix cores ----------------------
 hipError_t launch_mfma_probe(int shape, int lds_reads, int valu_per_mfma, float* sink,
