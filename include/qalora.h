@@ -236,6 +236,49 @@ int qalora_backward_kept(const qalora_desc* desc, int tokens, const void* dy, co
                          const float* A, const float* B, void* dx, int dx_dtype, float* dA,
                          float* dB, int accumulate, void* ws, size_t ws_bytes, void* stream);
 
+/* The linear with what follows it, applied in fp32 before the result is stored (y is rounded once):
+ *   z = x W~ + s (pool_g(x) A) B + bias;    y = act(z) * mul + residual.
+ * Each member may be absent (NULL; QALORA_ACT_NONE); an epilogue without any, or NULL, is the plain linear.
+ *   act       relu; silu(z) = z / (1 + exp(-z)); gelu(z) = z Phi(z); or its form by tanh,
+ *             0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3)))
+ *   bias      fp32 [d_out]
+ *   mul       bf16 [tokens, d_out]: with the up projection here, the gate's call gives a SwiGLU block's hidden activations
+ *   residual  [tokens, d_out] of y's type; it may be y itself (the residual stream is then updated in place)
+ *   z         out, bf16 [tokens, d_out]: z rounded, for qalora_epilogue_backward
+ * qalora_forward_epilogue is qalora_forward with it, or, where kept is not NULL, qalora_forward_keep;
+ * qalora_forward_deployed_epilogue is qalora_forward_deployed with it.  Same kernels, workspaces, precision of
+ * the product (few tokens: exact operands), limits and status word: y is what the epilogue makes of the sums that these calls
+ * round.  Backward: qalora_epilogue_backward, then qalora_backward on its dz. */
+enum qalora_act { QALORA_ACT_NONE = 0, QALORA_ACT_RELU = 1, QALORA_ACT_SILU = 2, QALORA_ACT_GELU = 3, QALORA_ACT_GELU_TANH = 4 };
+typedef struct qalora_epilogue {
+  int32_t act;
+  const float* bias;
+  const void* mul;
+  const void* residual;
+  void* z;
+} qalora_epilogue;
+int qalora_forward_epilogue(const qalora_desc* desc, int tokens, const void* x, const void* packed,
+                            const float* alpha, const float* beta, const float* A, const float* B,
+                            const qalora_epilogue* epilogue /* host, or NULL */, void* y, int y_dtype,
+                            void* kept /* or NULL */, void* ws, size_t ws_bytes, void* stream);
+int qalora_forward_deployed_epilogue(const qalora_desc* desc, int tokens, const void* x, const void* packed,
+                                     const void* deployed, const qalora_epilogue* epilogue /* host, or NULL */,
+                                     void* y, int y_dtype, void* ws, size_t ws_bytes, void* stream);
+
+/* Backward of the epilogue, at the z the forward kept:
+ *   dz = dy * mul * act'(z);   dmul = dy * act(z);   dbias = sum over the tokens of dz      (d residual = dy).
+ * dz is the dy of qalora_backward.  All [tokens, cols], cols a multiple of 8 (QALORA_EUNSUPPORTED otherwise); arithmetic in
+ * fp32, dz and dmul rounded to bf16, dbias the sum of the unrounded values.
+ * in : dy fp32 or bf16 per dy_dtype; z bf16, NULL allowed where neither act nor dmul needs it; mul bf16 or NULL
+ * out: dz, dmul bf16, dbias fp32 [cols]: at least one, the others NULL; dmul only with mul; a bf16 dz may be dy itself.
+ *      accumulate = 1 adds to dbias.  The slope of relu at zero is zero.
+ * ws: qalora_epilogue_backward_workspace_bytes(tokens, cols) bytes, needed for dbias.  Reruns are bit-identical; may be
+ * captured into a HIP graph. */
+size_t qalora_epilogue_backward_workspace_bytes(int tokens, int cols);
+int qalora_epilogue_backward(int act, int tokens, int cols, const void* dy, int dy_dtype, const void* z,
+                             const void* mul, void* dz, void* dmul, float* dbias, int accumulate, void* ws,
+                             size_t ws_bytes, void* stream);
+
 /* Several adapted linears that share their input x (q/k/v of an attention block; gate/up of a
  * SwiGLU MLP), evaluated as ONE wide layer: one pass over x (row scales, conversion, pooling --
  * pool_g(x) is the same for all of them), one dense launch over the concatenated columns, and

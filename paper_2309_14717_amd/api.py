@@ -40,6 +40,8 @@ EXPORTS = (
     "qalora_quantize_compensated",
     "qalora_backward_shared", "qalora_swiglu_forward_wide", "qalora_swiglu_backward_wide",
     "qalora_muon_workspace_bytes", "qalora_muon_step",
+    "qalora_forward_epilogue", "qalora_forward_deployed_epilogue",
+    "qalora_epilogue_backward_workspace_bytes", "qalora_epilogue_backward",
 )
 
 
@@ -117,6 +119,11 @@ def load() -> ctypes.CDLL:
     lib.qalora_adamw_workspace_bytes.restype = sz
     lib.qalora_adamw_workspace_bytes.argtypes = [i, vp]
     lib.qalora_adamw_step.argtypes = [vp, i, i, vp, vp, vp, vp, vp, i, vp, vp, sz, vp]
+    lib.qalora_forward_epilogue.argtypes = [cp, i, vp, vp, vp, vp, vp, vp, vp, vp, i, vp, vp, sz, vp]
+    lib.qalora_forward_deployed_epilogue.argtypes = [cp, i, vp, vp, vp, vp, vp, i, vp, sz, vp]
+    lib.qalora_epilogue_backward_workspace_bytes.restype = sz
+    lib.qalora_epilogue_backward_workspace_bytes.argtypes = [i, i]
+    lib.qalora_epilogue_backward.argtypes = [i, i, i, vp, i, vp, vp, vp, vp, vp, i, vp, sz, vp]
     lib.qalora_muon_workspace_bytes.restype = sz
     lib.qalora_muon_workspace_bytes.argtypes = [i, vp, vp]
     lib.qalora_muon_step.argtypes = [vp, i, vp, vp, vp, vp, vp, i, vp, sz, vp]
@@ -335,6 +342,88 @@ def forward_noalloc(desc: Desc, x, packed, alpha, beta, out_dtype=torch.float32,
     return y
 
 
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
+
+
+class Epilogue(ctypes.Structure):
+    """Mirror of ``qalora_epilogue``."""
+    _fields_ = [("act", ctypes.c_int32), ("bias", ctypes.c_void_p), ("mul", ctypes.c_void_p),
+                ("residual", ctypes.c_void_p), ("z", ctypes.c_void_p)]
+
+
+def _act(act):
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act: {act!r}, expected one of {', '.join(ACTIVATIONS)}")
+    return ACTIVATIONS[act]
+
+
+def _epilogue(T, d_out, dev, y, bias, act, mul, residual, z):
+    _need(bias, "bias", torch.float32, (d_out,), device=dev, optional=True)
+    _need(mul, "mul", torch.bfloat16, (T, d_out), device=dev, optional=True)
+    _need(residual, "residual", y.dtype, (T, d_out), device=dev, optional=True)
+    _need(z, "z", torch.bfloat16, (T, d_out), device=dev, optional=True)
+    address = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    return Epilogue(_act(act), address(bias), address(mul), address(residual), address(z))
+
+
+def forward_epilogue(desc: Desc, x, packed, alpha, beta, A=None, B=None, bias=None, act="none", mul=None,
+                     residual=None, keep_z=False, keep=False, out_dtype=torch.float32, ws=None, y=None, z=None, kept=None):
+    """forward() with y = act(x W~ + ... + bias) * mul + residual (see qalora_forward_epilogue).  ``act`` is one of
+    ACTIVATIONS; ``residual`` has y's type and may be the ``y`` that is passed.  Returns y; or (y, z, kept) with
+    ``keep_z`` (z in bf16, for epilogue_backward) or ``keep`` (the pooled activations, for backward_kept), None in the place
+    of the one not asked for."""
+    T, dev = _need_layer(desc, x, desc.d_in, packed, alpha, beta, A, B)
+    if y is None:
+        y = torch.empty((T, desc.d_out), dtype=out_dtype, device=dev)
+    _need_out(y, "y", T, desc.d_out, dev)
+    if keep_z and z is None:
+        z = torch.empty((T, desc.d_out), dtype=torch.bfloat16, device=dev)
+    if keep:
+        if kept is None:
+            kept = torch.empty(max(kept_bytes(desc, T), 16), dtype=torch.uint8, device=dev)
+        _need(kept, "kept", nbytes=kept_bytes(desc, T), device=dev)
+    epi = _epilogue(T, desc.d_out, dev, y, bias, act, mul, residual, z if keep_z else None)
+    ws, ws_bytes = _workspace(desc, T, OP_FORWARD, ws, dev)
+    rc = load().qalora_forward_epilogue(ctypes.byref(desc), T, _p(x), _p(packed), _p(alpha), _p(beta), _p(A), _p(B),
+                                        ctypes.byref(epi), _p(y), BF16 if y.dtype == torch.bfloat16 else F32,
+                                        _p(kept) if keep else None, _p(ws), ws_bytes, _stream())
+    _check(rc, "qalora_forward_epilogue")
+    return (y, z if keep_z else None, kept if keep else None) if keep or keep_z else y
+
+
+def epilogue_backward(dy, z=None, act="none", mul=None, want_dz=True, want_dbias=False, dz=None, dmul=None, dbias=None,
+                      accumulate=False, ws=None):
+    """Backward of the epilogue at the kept z (see qalora_epilogue_backward): (dz, dmul, dbias), None in the place of what
+    is not there: dmul without ``mul``, dbias unless wanted or given.  dz is the dy of backward(); the gradient of the
+    residual is dy itself."""
+    _need(dy, "dy")
+    if dy.dim() != 2 or dy.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"dy: {dy.dtype} {tuple(dy.shape)}, expected a float32 or bfloat16 matrix")
+    (T, cols), dev = dy.shape, dy.device
+    _need(z, "z", torch.bfloat16, (T, cols), device=dev, optional=True)
+    _need(mul, "mul", torch.bfloat16, (T, cols), device=dev, optional=True)
+    if dmul is not None and mul is None:
+        raise ValueError("dmul: given without mul")
+    if want_dz and dz is None:
+        dz = torch.empty((T, cols), dtype=torch.bfloat16, device=dev)
+    if mul is not None and dmul is None:
+        dmul = torch.empty((T, cols), dtype=torch.bfloat16, device=dev)
+    if want_dbias and dbias is None:
+        dbias = torch.zeros(cols, dtype=torch.float32, device=dev)
+    _need(dz, "dz", torch.bfloat16, (T, cols), device=dev, optional=True)
+    _need(dmul, "dmul", torch.bfloat16, (T, cols), device=dev, optional=True)
+    _need(dbias, "dbias", torch.float32, (cols,), device=dev, optional=True)
+    if ws is None and dbias is not None:
+        n = int(load().qalora_epilogue_backward_workspace_bytes(T, cols))
+        ws = torch.empty(max(n, 16), dtype=torch.uint8, device=dev)
+    _need(ws, "ws", device=dev, optional=True)
+    rc = load().qalora_epilogue_backward(_act(act), T, cols, _p(dy), BF16 if dy.dtype == torch.bfloat16 else F32, _p(z),
+                                         _p(mul), _p(dz), _p(dmul), _p(dbias), 1 if accumulate else 0, _p(ws),
+                                         0 if ws is None else ws.numel() * ws.element_size(), _stream())
+    _check(rc, "qalora_epilogue_backward")
+    return dz, dmul, dbias
+
+
 class Part(ctypes.Structure):
     """Mirror of ``qalora_part``."""
     _fields_ = [("d_out", ctypes.c_int32), ("rank", ctypes.c_int32), ("s", ctypes.c_float),
@@ -460,6 +549,28 @@ def forward_deployed(desc: Desc, x, deployed, packed=None, out_dtype=torch.float
     rc = load().qalora_forward_deployed(ctypes.byref(desc), T, _p(x), _p(packed), _p(deployed), _p(y),
                                         BF16 if y.dtype == torch.bfloat16 else F32, _p(ws), ws_bytes, _stream())
     _check(rc, "qalora_forward_deployed")
+    return y
+
+
+def forward_deployed_epilogue(desc: Desc, x, deployed, packed=None, bias=None, act="none", mul=None, residual=None,
+                              out_dtype=torch.float32, ws=None, y=None):
+    """forward_deployed() with the epilogue of forward_epilogue()."""
+    _need(x, "x", torch.bfloat16)
+    T, dev = x.shape[0], x.device
+    if check_desc(desc) == OK:
+        _need(x, "x", shape=(T, desc.d_in))
+        _need(deployed, "deployed", nbytes=int(load().qalora_deployed_bytes(ctypes.byref(desc))), device=dev)
+        if T > 4:
+            _need(packed, "packed", nbytes=packed_bytes(desc), device=dev)
+    if y is None:
+        y = torch.empty((T, desc.d_out), dtype=out_dtype, device=dev)
+    _need_out(y, "y", T, desc.d_out, dev)
+    epi = _epilogue(T, desc.d_out, dev, y, bias, act, mul, residual, None)
+    ws, ws_bytes = _workspace(desc, T, OP_FORWARD, ws, dev)
+    rc = load().qalora_forward_deployed_epilogue(ctypes.byref(desc), T, _p(x), _p(packed), _p(deployed), ctypes.byref(epi),
+                                                 _p(y), BF16 if y.dtype == torch.bfloat16 else F32, _p(ws), ws_bytes,
+                                                 _stream())
+    _check(rc, "qalora_forward_deployed_epilogue")
     return y
 
 

@@ -19,7 +19,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libqalora_hip.so")
 SOURCES = ["api.hip", "quantize.hip", "gemm_dq.hip", "adapter.hip", "smallt.hip", "smallt4.hip", "smallt4_f16.hip",
            "midt.hip", "glue.hip", "optim.hip", "probe.hip", "compensate.hip", "gemm_dq_192.hip",
-           "grads.hip", "muon.hip"]
+           "grads.hip", "muon.hip", "epilogue.hip", "gemm_dq_epi.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 LLVM = os.environ.get("HIP_CLANG_PATH", "/opt/rocm/llvm/bin")
 FLAGS = [
@@ -35,9 +35,9 @@ FLAGS = [
 # counter), and the adapter-gradient kernels, whose staging arrays once ended up in scratch
 # unnoticed (a local array the compiler does not promote to registers costs a round trip to
 # memory per element).
-NO_SCRATCH = {"gemm_dq.hip": "gemm_dq_kernel", "gemm_dq_192.hip": "gemm_dq_kernel", "midt.hip": "midt_kernel", "smallt.hip": "smallt_kernel", "smallt4.hip": "smallt4_kernel", "smallt4_f16.hip": "smallt4_kernel",
+NO_SCRATCH = {"gemm_dq.hip": "gemm_dq_kernel", "gemm_dq_192.hip": "gemm_dq_kernel", "gemm_dq_epi.hip": "gemm_dq_kernel", "midt.hip": "midt_kernel", "smallt.hip": "smallt_kernel", "smallt4.hip": "smallt4_kernel", "smallt4_f16.hip": "smallt4_kernel",
               "adapter.hip": ("front_kernel", "front_wide_kernel"), "grads.hip": ("z_kernel", "finish_kernel", "fused_kernel", "du_kernel", "db_kernel", "tail_kernel"),
-              "muon.hip": ("muon_start_kernel", "muon_pass_kernel")}
+              "muon.hip": ("muon_start_kernel", "muon_pass_kernel"), "epilogue.hip": "epilogue_back_kernel"}
 
 
 def _as_tuple(v):

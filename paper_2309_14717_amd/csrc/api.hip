@@ -195,6 +195,10 @@ inline size_t smallt_most(const qalora_desc& d, int tokens) {
   return most;
 }
 
+static_assert(ACT_NONE == (int)QALORA_ACT_NONE && ACT_RELU == (int)QALORA_ACT_RELU && ACT_SILU == (int)QALORA_ACT_SILU &&
+                  ACT_GELU == (int)QALORA_ACT_GELU && ACT_GELU_TANH == (int)QALORA_ACT_GELU_TANH,
+              "the header's activations");
+static_assert(MUON_MAX_TENSORS == QALORA_MUON_MAX_TENSORS && MUON_MAX_SHORT == QALORA_MUON_MAX_SHORT, "the header documents these limits");
 static_assert(MAX_PARTS == QALORA_MAX_PARTS, "the header documents this limit");
 static_assert(ST_STATUS_OFFSET == QALORA_WS_STATUS_OFFSET, "the header documents this offset");
 
@@ -350,14 +354,14 @@ struct PreparedFactors {  // made ahead of the call (deployment)
 static int forward_impl(const qalora_desc* d, int tokens, const void* x, const void* packed,
                         const float* alpha, const float* beta, const PartSpec& ps, void* y, int y_dtype,
                         void* kept, bool keep, void* ws, size_t ws_bytes, void* stream,
-                        const PreparedFactors* pre = nullptr);
+                        const PreparedFactors* pre = nullptr, const Epilogue* epi = nullptr);
 static int backward_impl(const qalora_desc* d, int tokens, const void* dy, const void* x,
                          const void* kept, bool use_kept, const void* packed, const float* alpha,
                          const float* beta, const PartSpec& ps, void* dx, int dx_dtype, int accumulate,
                          void* ws, size_t ws_bytes, void* stream);
 static int forward_mid(const qalora_desc& d, int tokens, const void* x, const void* packed, const float* alpha,
                        const float* beta, const void* fac16, const void* dep_stream, void* y, int y_dtype, void* ws,
-                       size_t ws_bytes, hipStream_t st);
+                       size_t ws_bytes, hipStream_t st, const Epilogue* epi = nullptr);
 
 // A single layer as one part over all its columns; exactly one of A, B null is an error the
 // caller has checked for.
@@ -498,7 +502,7 @@ static int mid_blocks(const qalora_desc& d, int tokens, size_t& scratch) {
 // Returns -1 where the kernel does not apply (nothing enqueued), else 0 or a positive error.
 static int forward_mid(const qalora_desc& d, int tokens, const void* x, const void* packed, const float* alpha,
                        const float* beta, const void* fac16, const void* dep_stream, void* y, int y_dtype, void* ws,
-                       size_t ws_bytes, hipStream_t st) {
+                       size_t ws_bytes, hipStream_t st, const Epilogue* epi) {
   size_t scratch = 0;  // for flags and partials: none (and no waits) where that is too little
   const int blocks = mid_blocks(d, tokens, scratch);
   if (blocks < 1) return -1;
@@ -531,13 +535,14 @@ static int forward_mid(const qalora_desc& d, int tokens, const void* x, const vo
   a.d_in = d.d_in;
   a.d_out = d.d_out;
   a.group = d.group;
+  if (epi) a.epi = *epi;
   return launch_midt(d.bits, a, blocks, st) == hipSuccess ? 0 : 1;
 }
 
 static int forward_impl(const qalora_desc* d, int tokens, const void* x, const void* packed,
                         const float* alpha, const float* beta, const PartSpec& ps, void* y, int y_dtype,
                         void* kept, bool keep, void* ws, size_t ws_bytes, void* stream,
-                        const PreparedFactors* pre) {
+                        const PreparedFactors* pre, const Epilogue* epi) {
   const int rc = qalora_check_desc(d);
   if (rc != QALORA_OK) return rc;
   if (tokens <= 0 || !x || !packed || !y) return QALORA_EINVAL;
@@ -575,6 +580,7 @@ static int forward_impl(const qalora_desc* d, int tokens, const void* x, const v
     a.d_in = d->d_in;
     a.d_out = d->d_out;
     a.group = d->group;
+    if (epi) a.epi = *epi;
     return launch_smallt(a, as_stream(stream)) == hipSuccess ? QALORA_OK : QALORA_EHIP;
   }
   const FwdPlan plan = plan_forward(*d, tokens);
@@ -586,7 +592,7 @@ static int forward_impl(const qalora_desc* d, int tokens, const void* x, const v
   const int L = d->d_in / d->group;
   if (!adapter)
     if (const int mrc = forward_mid(*d, tokens, x, packed, alpha, beta, nullptr, pre ? pre->stream : nullptr, y, y_dtype,
-                                    ws, plan.total, st);
+                                    ws, plan.total, st, epi);
         mrc >= 0)
       return mrc == 0 ? QALORA_OK : QALORA_EHIP;
 
@@ -634,7 +640,68 @@ static int forward_impl(const qalora_desc* d, int tokens, const void* x, const v
   g.ksplit = plan.gemm.ksplit;
   g.tile_rows = plan.gemm.tile_rows;
   g.partial = plan.gemm.ksplit > 1 ? reinterpret_cast<float*>(w + plan.gpart) : nullptr;
-  return launch_gemm_dq(d->bits, false, g, st) == hipSuccess ? QALORA_OK : QALORA_EHIP;
+  return launch_gemm_dq(d->bits, false, g, st, nullptr, epi) == hipSuccess ? QALORA_OK : QALORA_EHIP;
+}
+
+// The header's epilogue as the kernels take it; null: none.
+static int read_epilogue(const qalora_epilogue* from, Epilogue& e, const Epilogue** use) {
+  *use = nullptr;
+  if (!from) return QALORA_OK;
+  if (from->act < QALORA_ACT_NONE || from->act > QALORA_ACT_GELU_TANH) return QALORA_EINVAL;
+  if (misaligned(from->bias) || misaligned(from->mul) || misaligned(from->residual) || misaligned(from->z)) return QALORA_EALIGN;
+  e.bias = from->bias;
+  e.mul = static_cast<const uint16_t*>(from->mul);
+  e.residual = from->residual;
+  e.z = static_cast<uint16_t*>(from->z);
+  e.act = from->act;
+  e.on = from->act != QALORA_ACT_NONE || from->bias || from->mul || from->residual || from->z;
+  if (e.on) *use = &e;
+  return QALORA_OK;
+}
+
+int qalora_forward_epilogue(const qalora_desc* d, int tokens, const void* x, const void* packed, const float* alpha,
+                            const float* beta, const float* A, const float* B, const qalora_epilogue* epilogue, void* y,
+                            int y_dtype, void* kept, void* ws, size_t ws_bytes, void* stream) {
+  if ((A == nullptr) != (B == nullptr)) return QALORA_EINVAL;
+  Epilogue e{};
+  const Epilogue* use;
+  if (const int rc = read_epilogue(epilogue, e, &use); rc != QALORA_OK) return rc;
+  return forward_impl(d, tokens, x, packed, alpha, beta, single_part(d, A, B, nullptr, nullptr), y, y_dtype, kept,
+                      kept != nullptr, ws, ws_bytes, stream, nullptr, use);
+}
+
+size_t qalora_epilogue_backward_workspace_bytes(int tokens, int cols) {
+  if (tokens <= 0 || cols <= 0 || cols % 8 != 0) return 0;
+  return align_up(epilogue_back_floats(tokens, cols) * sizeof(float));
+}
+
+int qalora_epilogue_backward(int act, int tokens, int cols, const void* dy, int dy_dtype, const void* z, const void* mul,
+                             void* dz, void* dmul, float* dbias, int accumulate, void* ws, size_t ws_bytes, void* stream) {
+  if (act < QALORA_ACT_NONE || act > QALORA_ACT_GELU_TANH || tokens <= 0 || cols <= 0 || !dy) return QALORA_EINVAL;
+  if (dy_dtype != QALORA_F32 && dy_dtype != QALORA_BF16) return QALORA_EINVAL;
+  if (accumulate != 0 && accumulate != 1) return QALORA_EINVAL;
+  if (!dz && !dmul && !dbias) return QALORA_EINVAL;
+  if (dmul && !mul) return QALORA_EINVAL;
+  if (!z && (act != QALORA_ACT_NONE || dmul)) return QALORA_EINVAL;
+  if (misaligned(dy) || misaligned(z) || misaligned(mul) || misaligned(dz) || misaligned(dmul) || misaligned(dbias) ||
+      misaligned(ws))
+    return QALORA_EALIGN;
+  if (cols % 8 != 0) return QALORA_EUNSUPPORTED;
+  if (dbias && (!ws || ws_bytes < epilogue_back_floats(tokens, cols) * sizeof(float))) return QALORA_EWORKSPACE;
+  EpilogueBackArgs a{};
+  a.dy = dy;
+  a.z = static_cast<const uint16_t*>(z);
+  a.mul = static_cast<const uint16_t*>(mul);
+  a.dz = static_cast<uint16_t*>(dz);
+  a.dmul = static_cast<uint16_t*>(dmul);
+  a.dbias = dbias;
+  a.partial = static_cast<float*>(ws);
+  a.act = act;
+  a.dy_bf16 = dy_dtype == QALORA_BF16;
+  a.accumulate = accumulate;
+  a.rows = tokens;
+  a.cols = cols;
+  return launch_epilogue_backward(a, as_stream(stream)) == hipSuccess ? QALORA_OK : QALORA_EHIP;
 }
 
 static int backward_impl(const qalora_desc* d, int tokens, const void* dy, const void* x,
@@ -877,9 +944,9 @@ int qalora_deploy(const qalora_desc* d, const void* packed, const float* alpha, 
   return launch_factor_job(fj, as_stream(stream)) == hipSuccess ? QALORA_OK : QALORA_EHIP;
 }
 
-int qalora_forward_deployed(const qalora_desc* d, int tokens, const void* x, const void* packed,
-                            const void* deployed, void* y, int y_dtype, void* ws, size_t ws_bytes,
-                            void* stream) {
+static int forward_deployed_impl(const qalora_desc* d, int tokens, const void* x, const void* packed,
+                                 const void* deployed, void* y, int y_dtype, void* ws, size_t ws_bytes,
+                                 void* stream, const Epilogue* epi) {
   const int rc = qalora_check_desc(d);
   if (rc != QALORA_OK) return rc;
   if (tokens <= 0 || !x || !deployed || !y) return QALORA_EINVAL;
@@ -895,7 +962,7 @@ int qalora_forward_deployed(const qalora_desc* d, int tokens, const void* x, con
     const PreparedFactors pre{reinterpret_cast<const uint32_t*>(static_cast<const char*>(deployed) + l.words),
                               reinterpret_cast<const float*>(static_cast<const char*>(deployed) + l.inv), deployed};
     return forward_impl(d, tokens, x, packed, nullptr, nullptr, PartSpec{}, y, y_dtype, nullptr, false, ws,
-                        ws_bytes, stream, &pre);
+                        ws_bytes, stream, &pre, epi);
   }
   const size_t need = smallt_workspace(*d, tokens);
   if (!ws || ws_bytes < need) return QALORA_EWORKSPACE;
@@ -912,7 +979,23 @@ int qalora_forward_deployed(const qalora_desc* d, int tokens, const void* x, con
   a.d_in = d->d_in;
   a.d_out = d->d_out;
   a.group = d->group;
+  if (epi) a.epi = *epi;
   return launch_smallt4_deployed(a, as_stream(stream)) == hipSuccess ? QALORA_OK : QALORA_EHIP;
+}
+
+int qalora_forward_deployed(const qalora_desc* d, int tokens, const void* x, const void* packed,
+                            const void* deployed, void* y, int y_dtype, void* ws, size_t ws_bytes,
+                            void* stream) {
+  return forward_deployed_impl(d, tokens, x, packed, deployed, y, y_dtype, ws, ws_bytes, stream, nullptr);
+}
+
+int qalora_forward_deployed_epilogue(const qalora_desc* d, int tokens, const void* x, const void* packed,
+                                     const void* deployed, const qalora_epilogue* epilogue, void* y, int y_dtype,
+                                     void* ws, size_t ws_bytes, void* stream) {
+  Epilogue e{};
+  const Epilogue* use;
+  if (const int rc = read_epilogue(epilogue, e, &use); rc != QALORA_OK) return rc;
+  return forward_deployed_impl(d, tokens, x, packed, deployed, y, y_dtype, ws, ws_bytes, stream, use);
 }
 
 int qalora_pack_factors16(const qalora_desc* d, const float* alpha, const float* beta, void* factors16,

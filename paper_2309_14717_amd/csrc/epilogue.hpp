@@ -1,0 +1,94 @@
+// What follows a linear, applied before its result leaves the kernel that has it:
+//   z = (x W~' ) + bias;   y = act(z) * mul + residual        (z may be stored too, in bf16, for the backward)
+// All in fp32 on the fp32 result; y is rounded once.
+#pragma once
+#include "common.hpp"
+
+namespace qalora {
+
+enum Act { ACT_NONE = 0, ACT_RELU = 1, ACT_SILU = 2, ACT_GELU = 3, ACT_GELU_TANH = 4 };
+
+struct Epilogue {
+  const float* bias;     // [N], or null
+  const uint16_t* mul;   // bf16 [M, N], or null
+  const void* residual;  // [M, N] of y's type, or null
+  uint16_t* z;           // bf16 [M, N], or null
+  int act;
+  int on;                // whether there is anything to do
+};
+
+// 1 / (1 + exp(-v)); zero and one where that is what fp32 holds
+__device__ __forceinline__ float logistic(float v) { return __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
+constexpr float kTanhSlope = 1.5957691216057308f;  // 2 sqrt(2 / pi): 0.5 (1 + tanh(u)) = logistic(2 u)
+__device__ __forceinline__ float gelu_tanh_arg(float v) { return kTanhSlope * v * __builtin_fmaf(0.044715f * v, v, 1.0f); }
+
+// (relu keeps a NaN.  The normal distribution function by erfc, which keeps its relative precision for negative v.)
+__device__ __forceinline__ float act_value(int act, float v) {
+  switch (act) {
+    case ACT_RELU: return v < 0.0f ? 0.0f : v;
+    case ACT_SILU: return v * logistic(v);
+    case ACT_GELU: return 0.5f * v * erfcf(-0.70710678f * v);
+    case ACT_GELU_TANH: return v * logistic(gelu_tanh_arg(v));
+    default: return v;
+  }
+}
+
+// act(v) and its slope.  Beyond +-16 (silu: +-100) every slope is zero or one in fp32: the argument is held there, so that
+// no product of an overflow and a zero arises.  (Comparisons, not fmin and fmax, which would lose a NaN.)
+__device__ __forceinline__ float held(float v, float at) { return v > at ? at : (v < -at ? -at : v); }
+__device__ __forceinline__ void act_slope(int act, float v, float& value, float& slope) {
+  switch (act) {
+    case ACT_RELU:
+      value = v < 0.0f ? 0.0f : v;
+      slope = v > 0.0f ? 1.0f : 0.0f;
+      return;
+    case ACT_SILU: {
+      const float c = held(v, 100.0f), s = logistic(c);
+      value = v * s;
+      slope = s * __builtin_fmaf(c, 1.0f - s, 1.0f);
+      return;
+    }
+    case ACT_GELU: {
+      const float c = held(v, 16.0f), cdf = 0.5f * erfcf(-0.70710678f * c);
+      value = v * cdf;
+      slope = __builtin_fmaf(0.39894228f * c, __expf(-0.5f * c * c), cdf);
+      return;
+    }
+    case ACT_GELU_TANH: {
+      const float c = held(v, 16.0f), s = logistic(gelu_tanh_arg(c));
+      value = v * s;
+      slope = __builtin_fmaf(c * s * (1.0f - s), kTanhSlope * __builtin_fmaf(3.0f * 0.044715f * c, c, 1.0f), s);
+      return;
+    }
+    default:
+      value = v;
+      slope = 1.0f;
+  }
+}
+
+// Four neighbouring elements (the first at element `at`, column `col`; both multiples of four): y from the linear's sums.
+// Where residual is y itself, each is read here before the caller stores it.
+__device__ __forceinline__ f32x4 apply_epilogue(const Epilogue& e, f32x4 v, size_t at, int col, int out_bf16) {
+  typedef uint32_t pair __attribute__((ext_vector_type(2)));
+  if (e.bias) v += *reinterpret_cast<const f32x4*>(e.bias + col);
+  if (e.z) *reinterpret_cast<pair*>(e.z + at) = pair{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = act_value(e.act, v[k]);
+  if (e.mul) {
+    const pair m = *reinterpret_cast<const pair*>(e.mul + at);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] *= __uint_as_float((k & 1) ? m[k >> 1] & 0xffff0000u : m[k >> 1] << 16);
+  }
+  if (e.residual) {
+    if (out_bf16) {
+      const pair r = *reinterpret_cast<const pair*>(static_cast<const uint16_t*>(e.residual) + at);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] += __uint_as_float((k & 1) ? r[k >> 1] & 0xffff0000u : r[k >> 1] << 16);
+    } else {
+      v += *reinterpret_cast<const f32x4*>(static_cast<const float*>(e.residual) + at);
+    }
+  }
+  return v;
+}
+
+}  // namespace qalora

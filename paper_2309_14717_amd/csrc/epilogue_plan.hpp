@@ -1,0 +1,33 @@
+// Launch shape and workspace of the epilogue's backward (epilogue.hip).
+#pragma once
+#include <stddef.h>
+
+namespace qalora {
+
+constexpr int EB_THREADS = 256;
+constexpr int EB_MAX_LANES = 64;  // of eight columns each: a row of a block's tile is up to 1 KB of bf16
+
+struct EpilogueBackPlan {
+  int lanes;       // threads along a row (a power of two); the block takes EB_THREADS / lanes rows at a time
+  int col_blocks;
+  int row_blocks;  // each of `rows_per` rows
+  int rows_per;
+};
+inline EpilogueBackPlan epilogue_back_plan(int rows, int cols) {
+  EpilogueBackPlan p{};
+  const int eights = cols / 8;
+  p.lanes = EB_MAX_LANES;
+  while (p.lanes > 8 && p.lanes / 2 >= eights) p.lanes /= 2;
+  p.col_blocks = (eights + p.lanes - 1) / p.lanes;
+  const int at_once = EB_THREADS / p.lanes;
+  const int want = (2048 + p.col_blocks - 1) / p.col_blocks;  // eight blocks per compute unit
+  const int sweeps = rows / at_once + (rows % at_once ? 1 : 0);
+  const int sweeps_per = sweeps / want > 4 ? sweeps / want + 1 : 4;
+  p.rows_per = sweeps_per * at_once;
+  p.row_blocks = sweeps / sweeps_per + (sweeps % sweeps_per ? 1 : 0);
+  return p;
+}
+// The row blocks' shares of dbias.
+inline size_t epilogue_back_floats(int rows, int cols) { return (size_t)epilogue_back_plan(rows, cols).row_blocks * cols; }
+
+}  // namespace qalora

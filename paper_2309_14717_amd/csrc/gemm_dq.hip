@@ -35,7 +35,7 @@ static hipError_t launch_bits(int bits, bool bwd, const GemmArgs& a, hipStream_t
   return bwd ? launch_dir<2, true>(a, st, e0, e1) : launch_dir<2, false>(a, st, e0, e1);
 }
 
-hipError_t launch_gemm_dq(int bits, bool bwd, const GemmArgs& args, hipStream_t st, SplitSum* sum) {
+hipError_t launch_gemm_dq(int bits, bool bwd, const GemmArgs& args, hipStream_t st, SplitSum* sum, const Epilogue* epi) {
   GemmArgs a = args;
   const bool split = a.ksplit > 1;
   if (split) {  // slices write fp32 partials; the sum is converted afterwards
@@ -51,11 +51,14 @@ hipError_t launch_gemm_dq(int bits, bool bwd, const GemmArgs& args, hipStream_t 
   // (the product alone where the caller sums)
   const bool ride = !split && hook.start && hook.stop;
   if (hook.start && !ride) (void)hipEventRecord(hook.start, st);
-  hipError_t e = launch_bits(bits, bwd, a, st, ride ? hook.start : nullptr, ride ? hook.stop : nullptr);
+  const hipEvent_t e0 = ride ? hook.start : nullptr, e1 = ride ? hook.stop : nullptr;
+  hipError_t e = epi && !split ? launch_gemm_dq_epi(bits, GemmEpiArgs{a, *epi}, st, e0, e1) : launch_bits(bits, bwd, a, st, e0, e1);
   if (e == hipSuccess && split) {
     const SplitSum todo{a.partial, a.ksplit, (size_t)a.M * a.N / 4, args.out, args.out_bf16};  // N is a multiple of 8
     if (sum) {
       *sum = todo;
+    } else if (epi) {
+      e = launch_split_epilogue(todo, *epi, a.N, st);
     } else {
       split_reduce_kernel<<<(unsigned)((todo.n4 + 255) / 256), 256, 0, st>>>(todo);
       e = hipGetLastError();

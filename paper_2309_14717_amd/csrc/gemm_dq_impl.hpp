@@ -141,8 +141,9 @@ constexpr int gemm_min_waves(int bm, int nbits, bool bwd, bool fast) {
 // copies padded to whole row tiles): every per-lane global offset is a kernel-lifetime
 // constant and the K advance lives in scalar offsets, so the hot loop carries no vector
 // address arithmetic.  FAST = false keeps per-step, per-lane offsets with full edge handling.
-template <int NBITS, bool BWD, int BM, int BN, int WAVES_M, int WAVES_N, bool FAST>
-__global__ __launch_bounds__(NT, gemm_min_waves(BM, NBITS, BWD, FAST)) void gemm_dq_kernel(const GemmArgs p) {
+// Args: GemmArgs, or GemmEpiArgs for a forward product with an epilogue.
+template <int NBITS, bool BWD, int BM, int BN, int WAVES_M, int WAVES_N, bool FAST, typename Args = GemmArgs>
+__global__ __launch_bounds__(NT, gemm_min_waves(BM, NBITS, BWD, FAST)) void gemm_dq_kernel(const Args p) {
   static_assert(WAVES_M * WAVES_N == 8, "eight wavefronts per block");
   static_assert(BN == 256, "the dequantising producer assumes 256 columns");
   constexpr int WTM = BM / WAVES_M, WTN = BN / WAVES_N;
@@ -654,7 +655,67 @@ __global__ __launch_bounds__(NT, gemm_min_waves(BM, NBITS, BWD, FAST)) void gemm
     const int n = n0 + e_wn * WTN + b * 32 + (e_lane & 31);
     inv_n[b] = BWD ? p.n_scale[0] : (n < p.N ? p.n_scale[n] : 1.0f);
   }
-  auto epilogue = [&](auto as_bf16) {
+  // With an epilogue the tile is staged as fp32 whatever y's type, and a thread takes eight columns of a row, the same eight
+  // of every row it comes to: its share of the bias stays in registers.
+  [[maybe_unused]] auto epilogue_with = [&](const Epilogue& epi) {
+    constexpr int ROW = BN * 4 + 16;
+    constexpr int kLds = (A_STAGES * BM + 2 * BN) * 64 * 2;
+    constexpr int kPasses = ceil_div(BM * ROW + BM * 4, kLds);
+    constexpr int RP = BM / kPasses;
+    static_assert(BM % kPasses == 0 && RP * ROW + BM * 4 <= kLds && (RP % WTM == 0 || WTM % RP == 0), "a pass is whole or halved wave row-bands");
+    static_assert(RP % 32 == 0, "and whole rows of matrix instructions");
+    constexpr int CPR = BN / 8, ROWS_AT_ONCE = NT / CPR;
+    const int ch = e_tid % CPR, col = n0 + 8 * ch;
+    f32x4 bias[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
+    if (epi.bias && col < p.N) {
+      bias[0] = reinterpret_cast<const f32x4*>(epi.bias + col)[0];
+      bias[1] = reinterpret_cast<const f32x4*>(epi.bias + col)[1];
+    }
+    Epilogue rest = epi;
+    rest.bias = nullptr;
+    __syncthreads();  // row scales visible
+#pragma unroll
+    for (int pass = 0; pass < kPasses; ++pass) {
+      if (pass > 0) __syncthreads();  // the previous pass has been read out
+#pragma unroll
+      for (int a = 0; a < TM; ++a) {
+        const int rbase = e_wm * WTM + a * 32 - pass * RP;  // of this row of tiles, in the pass
+        if (rbase < 0 || rbase >= RP) continue;
+        f32x4 inv[4];
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4)
+          inv[g4] = *reinterpret_cast<const f32x4*>(inv_s + e_wm * WTM + a * 32 + 8 * g4 + 4 * (e_lane >> 5));
+#pragma unroll
+        for (int b = 0; b < TN; ++b) {
+          const int cl = e_wn * WTN + b * 32 + (e_lane & 31);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int rl = rbase + 8 * (r >> 2) + 4 * (e_lane >> 5) + (r & 3);
+            *reinterpret_cast<float*>(stage + rl * ROW + cl * 4) = acc[a][b][r] * inv[r >> 2][r & 3] * inv_n[b];
+          }
+        }
+      }
+      __syncthreads();
+#pragma unroll 2
+      for (int rl = e_tid / CPR; rl < RP; rl += ROWS_AT_ONCE) {
+        const int row = m0 + pass * RP + rl;
+        if (row >= p.M || col >= p.N) break;
+        const size_t at = (size_t)row * p.N + col;
+        const f32x4* s = reinterpret_cast<const f32x4*>(stage + rl * ROW + ch * 32);
+        const f32x4 y0 = apply_epilogue(rest, s[0] + bias[0], at, col, p.out_bf16);
+        const f32x4 y1 = apply_epilogue(rest, s[1] + bias[1], at + 4, col + 4, p.out_bf16);
+        if (p.out_bf16) {
+          *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + at) =
+              uint4{pack_bf16x2(y0[0], y0[1]), pack_bf16x2(y0[2], y0[3]), pack_bf16x2(y1[0], y1[1]), pack_bf16x2(y1[2], y1[3])};
+        } else {
+          f32x4* o = reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at);
+          o[0] = y0;
+          o[1] = y1;
+        }
+      }
+    }
+  };
+  [[maybe_unused]] auto epilogue = [&](auto as_bf16) {
     constexpr bool kBf16 = decltype(as_bf16)::value;
     constexpr int ES = kBf16 ? 2 : 4;
     constexpr int ROW = BN * ES + 16;  // staged row stride (+16: spreads rows over banks)
@@ -705,10 +766,14 @@ __global__ __launch_bounds__(NT, gemm_min_waves(BM, NBITS, BWD, FAST)) void gemm
       }
     }
   };
-  if (p.out_bf16)
-    epilogue(std::true_type{});
-  else
-    epilogue(std::false_type{});
+  if constexpr (std::is_same_v<Args, GemmEpiArgs>) {
+    epilogue_with(p.epi);
+  } else {
+    if (p.out_bf16)
+      epilogue(std::true_type{});
+    else
+      epilogue(std::false_type{});
+  }
   if (probe) {
     p.clock_probe[2] = (unsigned long long)clock64();
     p.clock_probe[3] = (unsigned long long)wall_clock64();
@@ -716,10 +781,10 @@ __global__ __launch_bounds__(NT, gemm_min_waves(BM, NBITS, BWD, FAST)) void gemm
   if (timeline) p.block_times[4 * blockIdx.x + 2] = (unsigned long long)wall_clock64();
 }
 
-template <int NBITS, bool BWD, int BM, int BN, int WAVES_M, int WAVES_N, bool FAST>
-static hipError_t launch_cfg(const GemmArgs& a, int ksplit, hipStream_t st, hipEvent_t ev_start = nullptr,
+template <int NBITS, bool BWD, int BM, int BN, int WAVES_M, int WAVES_N, bool FAST, typename Args = GemmArgs>
+static hipError_t launch_cfg(const Args& a, int ksplit, hipStream_t st, hipEvent_t ev_start = nullptr,
                              hipEvent_t ev_stop = nullptr) {
-  auto kern = gemm_dq_kernel<NBITS, BWD, BM, BN, WAVES_M, WAVES_N, FAST>;
+  auto kern = gemm_dq_kernel<NBITS, BWD, BM, BN, WAVES_M, WAVES_N, FAST, Args>;
   const size_t smem = (size_t)(gemm_a_stages(BM) * BM + 2 * BN) * 64 * sizeof(uint16_t);
   static std::atomic<uint64_t> granted{0};  // per instantiation
   if (hipError_t e = grant_dynamic_lds(reinterpret_cast<const void*>(kern), (int)smem, granted); e != hipSuccess)

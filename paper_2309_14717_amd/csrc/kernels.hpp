@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "epilogue.hpp"
+#include "epilogue_plan.hpp"
 #include "grads_plan.hpp"
 #include "muon_plan.hpp"
 
@@ -50,9 +52,16 @@ struct GemmArgs {
   int block_times_cap;              // stores wall-clock ticks at start, K loop end and end, and
                                     // the id of the XCD it ran on, [4 b .. 4 b + 3]
 };
-// `sum`: where given and K is split, the sum over the slices is not launched but described there.
+struct GemmEpiArgs : GemmArgs {
+  Epilogue epi;
+};
+// `sum`: where given and K is split, the sum over the slices is not launched but described there.  `epi` (forward): what is
+// applied to the product, by its own kernel or by the sum over the slices.
 struct SplitSum;
-hipError_t launch_gemm_dq(int bits, bool bwd, const GemmArgs& a, hipStream_t st, SplitSum* sum = nullptr);
+hipError_t launch_gemm_dq(int bits, bool bwd, const GemmArgs& a, hipStream_t st, SplitSum* sum = nullptr,
+                          const Epilogue* epi = nullptr);
+hipError_t launch_gemm_dq_epi(int bits, const GemmEpiArgs& a, hipStream_t st, hipEvent_t e0, hipEvent_t e1);  // K not split
+hipError_t launch_split_epilogue(const SplitSum& s, const Epilogue& epi, int cols, hipStream_t st);
 // Measurement aid: events recorded around the next launch_gemm_dq of each direction.
 struct ProfileHook {
   hipEvent_t start, stop;
@@ -87,6 +96,7 @@ struct SmallTArgs {
   int out_bf16;
   int T, d_in, d_out, group;
   int bits;  // 4, 3 or 2
+  Epilogue epi;
 };
 // Launch shape: blocks = slabs * parts; `halves` (1 or 2) is how many ways a block splits its
 // own chunks, which sets the slab width (512 or 256 columns).
@@ -135,6 +145,7 @@ struct MidTArgs {
   unsigned long long nonce;   // filled in by the launcher, unique per call
   int out_bf16;
   int T, d_in, d_out, group;
+  Epilogue epi;
 };
 hipError_t launch_midt(int bits, const MidTArgs& a, int blocks, hipStream_t st);  // nonce set here
 
@@ -294,6 +305,21 @@ struct OptHyper {
   int zero_grads;
 };
 hipError_t launch_adamw(const OptTensors& t, const OptHyper& h, float* partial, float* norm_out, hipStream_t st);
+
+// --- epilogue.hip: the backward of a linear's epilogue ---------------------------------
+struct EpilogueBackArgs {
+  const void* dy;       // [rows, cols] bf16 or fp32
+  const uint16_t* z;    // bf16 [rows, cols]; null: not needed
+  const uint16_t* mul;  // bf16 [rows, cols], or null
+  uint16_t* dz;         // bf16 [rows, cols], or null
+  uint16_t* dmul;       // bf16 [rows, cols], or null
+  float* dbias;         // [cols], or null
+  float* partial;       // epilogue_back_floats; needed for dbias
+  int act, dy_bf16, accumulate;
+  int rows, cols;
+  EpilogueBackPlan plan;  // filled in by the launcher
+};
+hipError_t launch_epilogue_backward(const EpilogueBackArgs& a, hipStream_t st);
 
 // --- muon.hip: the orthogonalised update of up to 32 matrices ------------------------------
 struct MuonHyper {

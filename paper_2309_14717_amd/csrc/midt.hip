@@ -323,8 +323,9 @@ __global__ __launch_bounds__(MT_THREADS) void midt_kernel(const MidTArgs p) {
         const int tok = 16 * deep + 4 * f_kb + r;
         if (tok < p.T) {
           const float iv = bad ? __builtin_nanf("") : inv[r];  // a wait ran out: make it loud
-          const f32x4 v = {sum[0][r] * iv, sum[1][r] * iv, sum[2][r] * iv, sum[3][r] * iv};
+          f32x4 v = {sum[0][r] * iv, sum[1][r] * iv, sum[2][r] * iv, sum[3][r] * iv};
           const size_t o = (size_t)tok * p.d_out + j0;
+          if (p.epi.on) v = apply_epilogue(p.epi, v, o, j0, p.out_bf16);
           if (p.out_bf16)
             *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + o) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
           else

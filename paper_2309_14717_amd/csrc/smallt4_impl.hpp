@@ -476,6 +476,7 @@ __global__ __launch_bounds__(S4_THREADS) void smallt4_kernel(const SmallTArgs p)
           f32x4 v = tot[k] + *reinterpret_cast<const f32x4*>(tile + r * SLAB_COLS + 4 * c4);
           if (bad) v = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};  // a wait ran out: make it loud
           const size_t o = (size_t)r * p.d_out + jj;
+          if (p.epi.on) v = apply_epilogue(p.epi, v, o, jj, p.out_bf16);
           if (p.out_bf16)
             *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + o) =
                 u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};

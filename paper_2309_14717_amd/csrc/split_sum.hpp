@@ -52,7 +52,7 @@ __device__ __forceinline__ f32x4 sum_slices(const f32x4* src, size_t stride, int
 // there it is the other way round (100 x 1024: 2.7 and 2.2 us); 128 x 4096, where the line lies, takes 4.1 us
 // either way.
 constexpr size_t kSumOneByOne = 128 * 1024;  // threads: two wavefronts on every SIMD
-__device__ __forceinline__ void split_sum_one(const SplitSum& s, size_t i) {
+__device__ __forceinline__ f32x4 split_sum_value(const SplitSum& s, size_t i) {
   const f32x4* src = reinterpret_cast<const f32x4*>(s.partial) + i;
   f32x4 v;
   if (s.n4 >= kSumOneByOne) {
@@ -61,10 +61,14 @@ __device__ __forceinline__ void split_sum_one(const SplitSum& s, size_t i) {
   } else {
     v = sum_slices(src, s.n4, s.slices);
   }
+  return v;
+}
+__device__ __forceinline__ void split_sum_store(const SplitSum& s, size_t i, const f32x4& v) {
   if (s.out_bf16)
     reinterpret_cast<uint2*>(s.out)[i] = uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
   else
     reinterpret_cast<f32x4*>(s.out)[i] = v;
 }
+__device__ __forceinline__ void split_sum_one(const SplitSum& s, size_t i) { split_sum_store(s, i, split_sum_value(s, i)); }
 
 }  // namespace qalora
