@@ -21,6 +21,7 @@
 // Everything is fp32: products by v_mfma_f32_16x16x4_f32, operands read from LDS 16 bytes a lane where the contraction
 // index is contiguous (G, P by their symmetry, and X in X X^T), the four values then being those of four instructions.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.hpp"
 #include "kernels.hpp"
@@ -48,36 +49,63 @@ __device__ __forceinline__ f32x4 rows_product(const float* rows_i, const float* 
   return acc;
 }
 
+// The tensor whose blocks the launch's block lies in.  (All starts are compared at once: a search that reads one after
+// the other waits for each, 0.15 us a tensor.)
+__device__ __forceinline__ int muon_find(const int (&first)[MUON_MAX_TENSORS]) {
+  int ti = 0;
+#pragma unroll
+  for (int i = 1; i < MUON_MAX_TENSORS; ++i) ti += (int)blockIdx.x >= first[i] ? 1 : 0;
+  return ti;
+}
 struct Where {
   const MuonTensor* t;
   int c0, c1;  // chunks
   int slice;
 };
 __device__ __forceinline__ Where muon_where(const MuonTable& table) {
-  int ti = 0;
-  while (ti + 1 < table.n && (int)blockIdx.x >= table.t[ti + 1].block0) ++ti;
+  const int ti = muon_find(table.block0);
   const MuonTensor& t = table.t[ti];
-  Where w{&t, 0, 0, (int)blockIdx.x - t.block0};
+  Where w{&t, 0, 0, (int)blockIdx.x - table.block0[ti]};
   w.c0 = w.slice * table.per_block;
   w.c1 = min(t.chunks, w.c0 + table.per_block);
   return w;
 }
 
-// f(element of the matrix, place in the chunk's LDS tile) over a chunk's elements, threads along memory
-template <int THREADS, typename Fn>
-__device__ __forceinline__ void each_element(const MuonTensor& t, int chunk, Fn&& f) {
+// A thread's share of a chunk of a [rows, cols] matrix: W neighbours in memory (4 where rows of it are whole 16-byte pieces,
+// else 1) at a time, f(k, element, place in the chunk's LDS tile, distance of the neighbours there) for the k-th of them.  The
+// count is a constant, so that all loads of a share are in flight together.
+template <int MAXT, int NT, int W, typename Fn>
+__device__ __forceinline__ void each_piece(const MuonTensor& t, int chunk, Fn&& f) {
   const int n0 = chunk * MUON_CHUNK;
-  if (t.rows <= t.cols) {
-    const int n = n0 + (threadIdx.x & 63);
-    if (n < t.cols)
-      for (int i = threadIdx.x >> 6; i < t.rows; i += THREADS / 64) f((size_t)i * t.cols + n, i * XLD + (threadIdx.x & 63));
-  } else {
-    const int count = min(MUON_CHUNK, t.rows - n0) * t.cols;
-    for (int e = threadIdx.x; e < count; e += THREADS) {
-      const int n = e / t.cols, i = e - n * t.cols;
-      f((size_t)n0 * t.cols + e, i * XLD + n);
-    }
+  const bool wide = t.rows <= t.cols;
+  const int per_row = wide ? MUON_CHUNK / W : t.cols / W, rows = wide ? t.rows : min(MUON_CHUNK, t.rows - n0);
+#pragma unroll
+  for (int k = 0; k < 16 * MAXT * MUON_CHUNK / (NT * W); ++k) {
+    const int e = threadIdx.x + NT * k;
+    const int r = wide ? e / (MUON_CHUNK / W) : e / per_row, c = W * (e - r * per_row);
+    if (r >= rows || (wide && n0 + c >= t.cols)) continue;
+    f(k, wide ? (size_t)r * t.cols + n0 + c : (size_t)(n0 + r) * t.cols + c, wide ? r * XLD + c : c * XLD + r, wide ? 1 : XLD);
   }
+}
+template <int W>
+struct Piece {
+  float v[W];
+};
+template <int W>
+__device__ __forceinline__ Piece<W> load_piece(const float* p) {
+  Piece<W> r;
+  if constexpr (W == 4) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(p);
+    for (int e = 0; e < 4; ++e) r.v[e] = v[e];
+  } else {
+    r.v[0] = *p;
+  }
+  return r;
+}
+template <int W>
+__device__ __forceinline__ void store_piece(float* p, const Piece<W>& r) {
+  if constexpr (W == 4) *reinterpret_cast<f32x4*>(p) = f32x4{r.v[0], r.v[1], r.v[2], r.v[3]};
+  else *p = r.v[0];
 }
 
 // A block's share of G from the chunks it has in LDS one after the other: tile wave + NW q of the upper tiles in acc[q].
@@ -132,13 +160,25 @@ __global__ __launch_bounds__(64 * muon_waves(MAXT)) void muon_start_kernel(const
       for (int e = threadIdx.x; e < 16 * t.tiles * XLD; e += NT) xs[e] = 0.0f;
       __syncthreads();
     }
-    each_element<NT>(t, c, [&](size_t at, int in_lds) {
-      const float g = t.g[at];
-      const float m = __builtin_fmaf(h.momentum, t.m[at], g);
-      t.m[at] = m;
-      if (h.zero_grads) t.g[at] = 0.0f;
-      xs[in_lds] = h.nesterov ? __builtin_fmaf(h.momentum, m, g) : m;
-    });
+    auto momentum = [&](auto width) {
+      constexpr int W = decltype(width)::value, K = 16 * MAXT * MUON_CHUNK / (NT * W);
+      Piece<W> g[K], m[K];
+      each_piece<MAXT, NT, W>(t, c, [&](int k, size_t at, int, int) {
+        g[k] = load_piece<W>(t.g + at);
+        m[k] = load_piece<W>(t.m + at);
+      });
+      each_piece<MAXT, NT, W>(t, c, [&](int k, size_t at, int in_lds, int step) {
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+          m[k].v[e] = __builtin_fmaf(h.momentum, m[k].v[e], g[k].v[e]);
+          xs[in_lds + e * step] = h.nesterov ? __builtin_fmaf(h.momentum, m[k].v[e], g[k].v[e]) : m[k].v[e];
+        }
+        store_piece<W>(t.m + at, m[k]);
+        if (h.zero_grads) store_piece<W>(t.g + at, Piece<W>{});
+      });
+    };
+    if (t.cols % 4 == 0) momentum(std::integral_constant<int, 4>{});
+    else momentum(std::integral_constant<int, 1>{});
     __syncthreads();
     f32x4* x = reinterpret_cast<f32x4*>(ws + t.x) + (size_t)c * t.tiles * 16 * (MUON_CHUNK / 4);
     for (int e = threadIdx.x; e < t.tiles * 16 * (MUON_CHUNK / 4); e += NT)
@@ -152,12 +192,11 @@ __global__ __launch_bounds__(64 * muon_waves(MAXT)) void muon_start_kernel(const
 // G = sum of the blocks' shares: 32 pieces of 16 bytes a block, their shares dealt to eight groups of threads.
 __global__ __launch_bounds__(256) void muon_reduce_kernel(const MuonTable table, float* ws) {
   __shared__ f32x4 part[8][32];
-  int ti = 0;
-  while (ti + 1 < table.n && (int)blockIdx.x >= table.t[ti + 1].reduce0) ++ti;
+  const int ti = muon_find(table.reduce0);
   const MuonTensor& t = table.t[ti];
   const int slices = (t.chunks + table.per_block - 1) / table.per_block;
   const int e = threadIdx.x & 31, group = threadIdx.x >> 5;
-  const size_t pieces = (size_t)muon_gram_tiles(t.tiles) * 64, at = (size_t)(blockIdx.x - t.reduce0) * 32 + e;
+  const size_t pieces = (size_t)muon_gram_tiles(t.tiles) * 64, at = (size_t)(blockIdx.x - table.reduce0[ti]) * 32 + e;
   const f32x4* src = reinterpret_cast<const f32x4*>(ws + t.partial) + at;
   const int per = (slices + 7) / 8, z0 = min(slices, group * per), z1 = min(slices, z0 + per);
   f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -184,6 +223,17 @@ __global__ __launch_bounds__(64 * muon_waves(MAXT)) void muon_pass_kernel(const 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lo = lane & 15, hi = lane >> 4;
   const int upper = muon_gram_tiles(t.tiles);
 
+  // The chunk that comes next, on its way: the first one while P is made, each later one while the one before is worked on.
+  constexpr int XK = 16 * MAXT * (MUON_CHUNK / 4) / NT;
+  f32x4 coming[XK];
+  const int pieces = t.tiles * 16 * (MUON_CHUNK / 4);
+  auto chunk_at = [&](int c) { return reinterpret_cast<f32x4*>(ws + t.x) + (size_t)c * pieces; };
+  auto request = [&](int c) {
+#pragma unroll
+    for (int k = 0; k < XK; ++k)
+      if (threadIdx.x + NT * k < (unsigned)pieces) coming[k] = chunk_at(c)[threadIdx.x + NT * k];
+  };
+
   // ---- P = a I + b G + c G^2 -------------------------------------------------------------
   constexpr int Q = (muon_gram_tiles(MAXT) + NW - 1) / NW;
   f32x4 g[Q];  // upper tiles wave + NW q: element (16 i + 4 hi + v, 16 j + lo)
@@ -197,6 +247,7 @@ __global__ __launch_bounds__(64 * muon_waves(MAXT)) void muon_pass_kernel(const 
 #pragma unroll
   for (int q = 0; q < Q; ++q)
     if (wave + NW * q < upper) g[q] = reinterpret_cast<const f32x4*>(ws + t.gram)[(wave + NW * q) * 64 + lane];
+  request(w.c0);
   float x_scale = 1.0f;
   if constexpr (FIRST) {
 #pragma unroll
@@ -239,10 +290,13 @@ __global__ __launch_bounds__(64 * muon_waves(MAXT)) void muon_pass_kernel(const 
   Gram<MAXT, NW> gram(t.tiles, wave, lane);
   const int col = 16 * (wave & 3) + lo, tile0 = 4 * (wave >> 2);  // four row tiles of sixteen columns a wavefront
   for (int c = w.c0; c < w.c1; ++c) {
-    f32x4* x = reinterpret_cast<f32x4*>(ws + t.x) + (size_t)c * t.tiles * 16 * (MUON_CHUNK / 4);
-    for (int e = threadIdx.x; e < t.tiles * 16 * (MUON_CHUNK / 4); e += NT)
-      *reinterpret_cast<f32x4*>(xs + (e >> 4) * XLD + 4 * (e & 15)) = x[e];
+#pragma unroll
+    for (int k = 0; k < XK; ++k) {
+      const int e = threadIdx.x + NT * k;
+      if (e < pieces) *reinterpret_cast<f32x4*>(xs + (e >> 4) * XLD + 4 * (e & 15)) = coming[k];
+    }
     __syncthreads();
+    if (c + 1 < w.c1) request(c + 1);
     f32x4 acc[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) acc[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -266,10 +320,20 @@ __global__ __launch_bounds__(64 * muon_waves(MAXT)) void muon_pass_kernel(const 
         for (int e = 0; e < 4; ++e) xs[(16 * (tile0 + k) + 4 * hi + e) * XLD + col] = acc[k][e];
     __syncthreads();
     if constexpr (LAST) {
-      each_element<NT>(t, c, [&](size_t at, int in_lds) { t.p[at] = __builtin_fmaf(t.p[at], h.decay, -t.step_size * xs[in_lds]); });
+      auto update = [&](auto width) {
+        constexpr int W = decltype(width)::value, K = 16 * MAXT * MUON_CHUNK / (NT * W);
+        Piece<W> p[K];
+        each_piece<MAXT, NT, W>(t, c, [&](int k, size_t at, int, int) { p[k] = load_piece<W>(t.p + at); });
+        each_piece<MAXT, NT, W>(t, c, [&](int k, size_t at, int in_lds, int step) {
+#pragma unroll
+          for (int e = 0; e < W; ++e) p[k].v[e] = __builtin_fmaf(p[k].v[e], h.decay, -t.step_size * xs[in_lds + e * step]);
+          store_piece<W>(t.p + at, p[k]);
+        });
+      };
+      if (t.cols % 4 == 0) update(std::integral_constant<int, 4>{});
+      else update(std::integral_constant<int, 1>{});
     } else {
-      for (int e = threadIdx.x; e < t.tiles * 16 * (MUON_CHUNK / 4); e += NT)
-        x[e] = *reinterpret_cast<const f32x4*>(xs + (e >> 4) * XLD + 4 * (e & 15));
+      for (int e = threadIdx.x; e < pieces; e += NT) chunk_at(c)[e] = *reinterpret_cast<const f32x4*>(xs + (e >> 4) * XLD + 4 * (e & 15));
       gram.add(xs, t.tiles, wave);
     }
     __syncthreads();  // the next chunk overwrites these columns

@@ -15,8 +15,6 @@ struct MuonTensor {
   int rows, cols;
   int tiles;             // 16-row tiles of the shorter side
   int chunks;            // of the longer side
-  int block0;            // first block of the launches over X; blocks of `per_block` chunks
-  int reduce0;           // first block of the launch that adds the blocks' Gram matrices
   float step_size;       // lr times the shape's scale
   size_t x;              // floats from the workspace's start: X as [chunks][16 tiles][MUON_CHUNK]
   size_t gram;           // the Gram matrix: upper 16 x 16 tiles, as MuonGram stores them
@@ -24,6 +22,8 @@ struct MuonTensor {
 };
 struct MuonTable {
   int n, blocks, reduce_blocks, per_block, max_tiles;
+  int block0[MUON_MAX_TENSORS];   // first block of the launches over X; blocks of `per_block` chunks
+  int reduce0[MUON_MAX_TENSORS];  // first block of the launch that adds the blocks' Gram matrices
   MuonTensor t[MUON_MAX_TENSORS];
 };
 constexpr int muon_gram_tiles(int tiles) { return tiles * (tiles + 1) / 2; }
@@ -62,8 +62,8 @@ inline size_t muon_table(int n, const int32_t* rows, const int32_t* cols, MuonTa
     MuonTensor& t = table.t[i];
     const int blocks = (t.chunks + table.per_block - 1) / table.per_block;
     const size_t gram = (size_t)muon_gram_tiles(t.tiles) * 256;
-    t.block0 = table.blocks;
-    t.reduce0 = table.reduce_blocks;
+    table.block0[i] = table.blocks;
+    table.reduce0[i] = table.reduce_blocks;
     table.blocks += blocks;
     table.reduce_blocks += muon_gram_tiles(t.tiles) * MUON_REDUCE_BLOCKS_PER_TILE;
     t.x = floats;
@@ -73,6 +73,7 @@ inline size_t muon_table(int n, const int32_t* rows, const int32_t* cols, MuonTa
     t.partial = floats;
     floats += (size_t)blocks * gram;
   }
+  for (int i = n; i < MUON_MAX_TENSORS; ++i) table.block0[i] = table.reduce0[i] = INT32_MAX;
   return floats;
 }
 

@@ -22,7 +22,7 @@ extern "C" void totals(long long* out) {
 }
 extern "C" void tensor(int i, long long* out) {
   const MuonTensor& t = table.t[i];
-  out[0] = t.tiles; out[1] = t.chunks; out[2] = t.block0; out[3] = t.reduce0;
+  out[0] = t.tiles; out[1] = t.chunks; out[2] = table.block0[i]; out[3] = table.reduce0[i];
   out[4] = (long long)t.x; out[5] = (long long)t.gram; out[6] = (long long)t.partial;
 }
 """
