@@ -139,7 +139,9 @@ _NATIVE_ENTRIES = (
     "qalora_kept_bytes", "qalora_forward_keep", "qalora_backward", "qalora_backward_kept", "qalora_deployed_bytes",
     "qalora_forward_deployed", "qalora_forward_factors16", "qalora_adamw_step", "qalora_shared_kept_bytes",
     "qalora_shared_workspace_bytes", "qalora_forward_shared", "qalora_backward_shared", "qalora_swiglu_forward_wide",
-    "qalora_swiglu_backward_wide")
+    "qalora_swiglu_backward_wide", "qalora_forward_epilogue", "qalora_forward_deployed_epilogue",
+    "qalora_epilogue_backward", "qalora_epilogue_backward_workspace_bytes", "qalora_muon_step",
+    "qalora_muon_workspace_bytes")
 
 
 def _bind_native():
@@ -153,7 +155,7 @@ def _bind_native():
         raise RuntimeError(f"{path} not found: build it first (python -m paper_2309_14717_amd.build)")
     from . import _native as native
     native.bind({name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _NATIVE_ENTRIES}, _check,
-                Desc, AdamW)
+                Desc, AdamW, Muon)
     _native = native
 
 
@@ -189,6 +191,11 @@ def _p(t):
 
 def _stream():
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+def _on(dev):
+    """The device of a call's tensors as the current one, whose stream the call then takes."""
+    return torch.cuda.device(dev)
 
 
 def _check(rc, where):
@@ -372,6 +379,10 @@ def forward_epilogue(desc: Desc, x, packed, alpha, beta, A=None, B=None, bias=No
     ACTIVATIONS; ``residual`` has y's type and may be the ``y`` that is passed.  Returns y; or (y, z, kept) with
     ``keep_z`` (z in bf16, for epilogue_backward) or ``keep`` (the pooled activations, for backward_kept), None in the place
     of the one not asked for."""
+    out = _fast().forward_epilogue(desc, x, packed, alpha, beta, A, B, bias, ACTIVATIONS.get(act), mul, residual, keep_z, keep,
+                                   out_dtype, ws, y, z, kept)
+    if out is not None:
+        return out
     T, dev = _need_layer(desc, x, desc.d_in, packed, alpha, beta, A, B)
     if y is None:
         y = torch.empty((T, desc.d_out), dtype=out_dtype, device=dev)
@@ -384,9 +395,10 @@ def forward_epilogue(desc: Desc, x, packed, alpha, beta, A=None, B=None, bias=No
         _need(kept, "kept", nbytes=kept_bytes(desc, T), device=dev)
     epi = _epilogue(T, desc.d_out, dev, y, bias, act, mul, residual, z if keep_z else None)
     ws, ws_bytes = _workspace(desc, T, OP_FORWARD, ws, dev)
-    rc = load().qalora_forward_epilogue(ctypes.byref(desc), T, _p(x), _p(packed), _p(alpha), _p(beta), _p(A), _p(B),
-                                        ctypes.byref(epi), _p(y), BF16 if y.dtype == torch.bfloat16 else F32,
-                                        _p(kept) if keep else None, _p(ws), ws_bytes, _stream())
+    with _on(dev):
+        rc = load().qalora_forward_epilogue(ctypes.byref(desc), T, _p(x), _p(packed), _p(alpha), _p(beta), _p(A), _p(B),
+                                            ctypes.byref(epi), _p(y), BF16 if y.dtype == torch.bfloat16 else F32,
+                                            _p(kept) if keep else None, _p(ws), ws_bytes, _stream())
     _check(rc, "qalora_forward_epilogue")
     return (y, z if keep_z else None, kept if keep else None) if keep or keep_z else y
 
@@ -396,6 +408,9 @@ def epilogue_backward(dy, z=None, act="none", mul=None, want_dz=True, want_dbias
     """Backward of the epilogue at the kept z (see qalora_epilogue_backward): (dz, dmul, dbias), None in the place of what
     is not there: dmul without ``mul``, dbias unless wanted or given.  dz is the dy of backward(); the gradient of the
     residual is dy itself."""
+    out = _fast().epilogue_backward(dy, z, ACTIVATIONS.get(act), mul, want_dz, want_dbias, dz, dmul, dbias, accumulate, ws)
+    if out is not None:
+        return out
     _need(dy, "dy")
     if dy.dim() != 2 or dy.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError(f"dy: {dy.dtype} {tuple(dy.shape)}, expected a float32 or bfloat16 matrix")
@@ -417,9 +432,11 @@ def epilogue_backward(dy, z=None, act="none", mul=None, want_dz=True, want_dbias
         n = int(load().qalora_epilogue_backward_workspace_bytes(T, cols))
         ws = torch.empty(max(n, 16), dtype=torch.uint8, device=dev)
     _need(ws, "ws", device=dev, optional=True)
-    rc = load().qalora_epilogue_backward(_act(act), T, cols, _p(dy), BF16 if dy.dtype == torch.bfloat16 else F32, _p(z),
-                                         _p(mul), _p(dz), _p(dmul), _p(dbias), 1 if accumulate else 0, _p(ws),
-                                         0 if ws is None else ws.numel() * ws.element_size(), _stream())
+    act = _act(act)
+    with _on(dev):
+        rc = load().qalora_epilogue_backward(act, T, cols, _p(dy), BF16 if dy.dtype == torch.bfloat16 else F32, _p(z),
+                                             _p(mul), _p(dz), _p(dmul), _p(dbias), 1 if accumulate else 0, _p(ws),
+                                             0 if ws is None else ws.numel() * ws.element_size(), _stream())
     _check(rc, "qalora_epilogue_backward")
     return dz, dmul, dbias
 
@@ -555,6 +572,10 @@ def forward_deployed(desc: Desc, x, deployed, packed=None, out_dtype=torch.float
 def forward_deployed_epilogue(desc: Desc, x, deployed, packed=None, bias=None, act="none", mul=None, residual=None,
                               out_dtype=torch.float32, ws=None, y=None):
     """forward_deployed() with the epilogue of forward_epilogue()."""
+    out = _fast().forward_deployed_epilogue(desc, x, deployed, packed, bias, ACTIVATIONS.get(act), mul, residual, out_dtype, ws,
+                                            y)
+    if out is not None:
+        return out
     _need(x, "x", torch.bfloat16)
     T, dev = x.shape[0], x.device
     if check_desc(desc) == OK:
@@ -567,9 +588,10 @@ def forward_deployed_epilogue(desc: Desc, x, deployed, packed=None, bias=None, a
     _need_out(y, "y", T, desc.d_out, dev)
     epi = _epilogue(T, desc.d_out, dev, y, bias, act, mul, residual, None)
     ws, ws_bytes = _workspace(desc, T, OP_FORWARD, ws, dev)
-    rc = load().qalora_forward_deployed_epilogue(ctypes.byref(desc), T, _p(x), _p(packed), _p(deployed), ctypes.byref(epi),
-                                                 _p(y), BF16 if y.dtype == torch.bfloat16 else F32, _p(ws), ws_bytes,
-                                                 _stream())
+    with _on(dev):
+        rc = load().qalora_forward_deployed_epilogue(ctypes.byref(desc), T, _p(x), _p(packed), _p(deployed),
+                                                     ctypes.byref(epi), _p(y), BF16 if y.dtype == torch.bfloat16 else F32,
+                                                     _p(ws), ws_bytes, _stream())
     _check(rc, "qalora_forward_deployed_epilogue")
     return y
 
@@ -805,6 +827,8 @@ def muon_workspace_bytes(tensors) -> int:
 def muon_step(hp: Muon, params, grads, momentum, zero_grads=False, ws=None):
     """One orthogonalised step (see qalora_muon_step) over lists of fp32 device matrices, one side of each at most
     128; ``params`` and ``momentum`` are updated in place."""
+    if _fast().muon_step(hp, params, grads, momentum, zero_grads, ws):
+        return
     n = len(params)
     if n == 0:
         raise ValueError("params: no tensors")
@@ -821,9 +845,10 @@ def muon_step(hp: Muon, params, grads, momentum, zero_grads=False, ws=None):
     if ws is None:
         ws = torch.empty(max(muon_workspace_bytes(params), 16), dtype=torch.uint8, device=params[0].device)
     _need(ws, "ws", device=params[0].device)
-    rc = load().qalora_muon_step(ctypes.byref(hp), n, ptrs[0], ptrs[1], ptrs[2], rows.buffer_info()[0],
-                                 cols.buffer_info()[0], 1 if zero_grads else 0, _p(ws), ws.numel() * ws.element_size(),
-                                 _stream())
+    with _on(params[0].device):
+        rc = load().qalora_muon_step(ctypes.byref(hp), n, ptrs[0], ptrs[1], ptrs[2], rows.buffer_info()[0],
+                                     cols.buffer_info()[0], 1 if zero_grads else 0, _p(ws), ws.numel() * ws.element_size(),
+                                     _stream())
     _check(rc, "qalora_muon_step")
 
 

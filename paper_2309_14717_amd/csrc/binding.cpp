@@ -9,6 +9,7 @@
 // tokens 56 us for 38 us on the GPU, AdamW over 14 tensors 31 for 20).
 #include <Python.h>
 
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
@@ -32,12 +33,14 @@ struct Library {
   X(qalora_kept_bytes) X(qalora_forward_keep) X(qalora_backward) X(qalora_backward_kept) X(qalora_deployed_bytes)     \
   X(qalora_forward_deployed) X(qalora_forward_factors16) X(qalora_adamw_step) X(qalora_shared_kept_bytes)             \
   X(qalora_shared_workspace_bytes) X(qalora_forward_shared) X(qalora_backward_shared) X(qalora_swiglu_forward_wide)   \
-  X(qalora_swiglu_backward_wide)
+  X(qalora_swiglu_backward_wide) X(qalora_forward_epilogue) X(qalora_forward_deployed_epilogue)                        \
+  X(qalora_epilogue_backward) X(qalora_epilogue_backward_workspace_bytes) X(qalora_muon_step) X(qalora_muon_workspace_bytes)
 #define QALORA_MEMBER(name) decltype(&::name) name = nullptr;
   QALORA_ENTRIES(QALORA_MEMBER)
 } lib;
 PyObject* raise_status = nullptr;  // api.py: (status, entry point) -> raises
-PyObject *desc_type = nullptr, *adamw_type = nullptr;  // api.py's mirrors of qalora_desc and qalora_adamw
+// api.py's mirrors of qalora_desc, qalora_adamw and qalora_muon
+PyObject *desc_type = nullptr, *adamw_type = nullptr, *muon_type = nullptr;
 bool bound = false;
 
 // The operands of one call, held until it returns (a list they came in can change while the interpreter lock is
@@ -144,6 +147,18 @@ struct Call {
       return at::empty({(int64_t)std::max<size_t>(size, 16)}, at::TensorOptions().dtype(at::kByte).device(dev));
     const at::Tensor* t = tensor(o);
     return t ? *t : at::Tensor();
+  }
+  // the call's device is the current one (elsewhere api.py makes it so first)
+  void on_current_device() { need(ok && dev.index() == c10::hip::current_device()); }
+  int integer(PyObject* o) {
+    if (!ok || !PyLong_CheckExact(o)) {
+      ok = false;
+      return 0;
+    }
+    const long v = PyLong_AsLong(o);
+    if (PyErr_Occurred()) PyErr_Clear(), ok = false;
+    need(v >= INT32_MIN && v <= INT32_MAX);
+    return (int)v;
   }
   bool truth(PyObject* o) {
     const int v = PyObject_IsTrue(o);
@@ -594,10 +609,175 @@ FASTCALL(adamw_step, 9)
   Py_RETURN_TRUE;
 FASTCALL_END
 
-// bind({entry point: address}, raise_status, Desc, AdamW)
+// The epilogue of a forward whose output is `y`, [c.T, d_out] of type `code`.
+qalora_epilogue epilogue(Call& c, PyObject* bias, PyObject* act, PyObject* mul, PyObject* residual, int code) {
+  qalora_epilogue e{};
+  e.act = c.integer(act);
+  if (c.ok && bias != Py_None) {
+    const at::Tensor* t = c.tensor(bias);
+    c.need(t && t->scalar_type() == at::kFloat && t->dim() == 1 && t->size(0) == c.desc.d_out);
+    if (c.ok) e.bias = f32(t->data_ptr());
+  }
+  if (c.ok && mul != Py_None) e.mul = c.matrix(mul, at::kBFloat16, c.T, c.desc.d_out);
+  if (c.ok && residual != Py_None)
+    e.residual = c.matrix(residual, code == QALORA_BF16 ? at::kBFloat16 : at::kFloat, c.T, c.desc.d_out);
+  return e;
+}
+
+// desc, x, packed, alpha, beta, A, B, bias, act, mul, residual, keep_z, keep, out_dtype, ws, y, z, kept
+FASTCALL(forward_epilogue, 18)
+  Call c;
+  c.layer(a[0]);
+  void* x = c.activations(a[1], c.desc.d_in);
+  c.on_current_device();
+  Weights w = weights(c, a[2], a[3], a[4]);
+  adapter(c, a[5], a[6], w);
+  const bool keep_z = c.truth(a[11]), keep = c.truth(a[12]);
+  c.need(!keep || w.A);
+  int code = 0;
+  const at::Tensor y = c.out(a[15], a[13], c.T, c.desc.d_out, code);
+  qalora_epilogue e = epilogue(c, a[7], a[8], a[9], a[10], code);
+  PLAIN(c);
+  at::Tensor z, kept;
+  if (keep_z) {
+    if (a[16] != Py_None) c.matrix(a[16], at::kBFloat16, c.T, c.desc.d_out);
+    PLAIN(c);
+    z = a[16] != Py_None ? THPVariable_Unpack(a[16])
+                         : at::empty({c.T, c.desc.d_out}, at::TensorOptions().dtype(at::kBFloat16).device(c.dev));
+    e.z = z.data_ptr();
+  }
+  if (keep) {
+    const size_t kb = lib.qalora_kept_bytes(&c.desc, (int)c.T);
+    kept = c.scratch(a[17], kb);
+    c.need(c.ok && (size_t)kept.nbytes() >= kb);
+  }
+  const at::Tensor ws = c.scratch(a[14], a[14] == Py_None ? lib.qalora_workspace_bytes(&c.desc, (int)c.T, QALORA_OP_FORWARD) : 0);
+  PLAIN(c);
+  void* st = stream();
+  if (!run("qalora_forward_epilogue", lib.qalora_forward_epilogue, &c.desc, (int)c.T, x, w.packed, f32(w.alpha), f32(w.beta),
+           f32(w.A), f32(w.B), &e, y.data_ptr(), code, keep ? kept.data_ptr() : nullptr, ws.data_ptr(), ws.nbytes(), st))
+    return nullptr;
+  if (!keep && !keep_z) return given_or(a[15], y);
+  return tuple({given_or(a[15], y), keep_z ? given_or(a[16], z) : Py_NewRef(Py_None),
+                keep ? given_or(a[17], kept) : Py_NewRef(Py_None)});
+FASTCALL_END
+
+// desc, x, deployed, packed, bias, act, mul, residual, out_dtype, ws, y
+FASTCALL(forward_deployed_epilogue, 11)
+  Call c;
+  c.layer(a[0]);
+  void* x = c.activations(a[1], c.desc.d_in);
+  c.on_current_device();
+  PLAIN(c);
+  const size_t need = lib.qalora_deployed_bytes(&c.desc);
+  c.need(need > 0);
+  void* deployed = c.bytes(a[2], need);
+  void* packed = nullptr;
+  if (c.ok && (a[3] != Py_None || c.T > QALORA_DEPLOYED_STREAM_TOKENS))
+    packed = c.bytes(a[3], c.T > QALORA_DEPLOYED_STREAM_TOKENS ? lib.qalora_packed_bytes(&c.desc) : 0);
+  int code = 0;
+  const at::Tensor y = c.out(a[10], a[8], c.T, c.desc.d_out, code);
+  const qalora_epilogue e = epilogue(c, a[4], a[5], a[6], a[7], code);
+  PLAIN(c);
+  const at::Tensor ws = c.scratch(a[9], a[9] == Py_None ? lib.qalora_workspace_bytes(&c.desc, (int)c.T, QALORA_OP_FORWARD) : 0);
+  PLAIN(c);
+  void* st = stream();
+  if (!run("qalora_forward_deployed_epilogue", lib.qalora_forward_deployed_epilogue, &c.desc, (int)c.T, x, packed, deployed,
+           &e, y.data_ptr(), code, ws.data_ptr(), ws.nbytes(), st))
+    return nullptr;
+  return given_or(a[10], y);
+FASTCALL_END
+
+// dy, z, act, mul, want_dz, want_dbias, dz, dmul, dbias, accumulate, ws
+FASTCALL(epilogue_backward, 11)
+  Call c;
+  const at::Tensor* dy = c.tensor(a[0], true);
+  c.need(dy && dy->dim() == 2 && dy->size(0) > 0 && dy->size(0) <= INT32_MAX && dy->size(1) > 0 && dy->size(1) <= INT32_MAX);
+  c.on_current_device();
+  PLAIN(c);
+  const int dtype = c.dtype_of(dy->scalar_type());
+  const int64_t T = dy->size(0), cols = dy->size(1);
+  void* z = a[1] != Py_None ? c.matrix(a[1], at::kBFloat16, T, cols) : nullptr;
+  const int act = c.integer(a[2]);
+  void* mul = a[3] != Py_None ? c.matrix(a[3], at::kBFloat16, T, cols) : nullptr;
+  const bool want_dz = c.truth(a[4]), want_dbias = c.truth(a[5]), acc = c.truth(a[9]);
+  c.need(a[7] == Py_None || mul);
+  if (a[6] != Py_None) c.matrix(a[6], at::kBFloat16, T, cols);
+  if (a[7] != Py_None) c.matrix(a[7], at::kBFloat16, T, cols);
+  if (c.ok && a[8] != Py_None) {
+    const at::Tensor* t = c.tensor(a[8]);
+    c.need(t && t->scalar_type() == at::kFloat && t->dim() == 1 && t->size(0) == cols);
+  }
+  PLAIN(c);
+  const auto opts = at::TensorOptions().device(c.dev);
+  at::Tensor dz, dmul, dbias, ws;
+  if (a[6] != Py_None) dz = THPVariable_Unpack(a[6]);
+  else if (want_dz) dz = at::empty({T, cols}, opts.dtype(at::kBFloat16));
+  if (a[7] != Py_None) dmul = THPVariable_Unpack(a[7]);
+  else if (mul) dmul = at::empty({T, cols}, opts.dtype(at::kBFloat16));
+  if (a[8] != Py_None) dbias = THPVariable_Unpack(a[8]);
+  else if (want_dbias) dbias = acc ? at::zeros({cols}, opts.dtype(at::kFloat)) : at::empty({cols}, opts.dtype(at::kFloat));
+  if (a[10] != Py_None) {
+    const at::Tensor* t = c.tensor(a[10]);
+    PLAIN(c);
+    ws = *t;
+  } else if (dbias.defined()) {
+    ws = c.scratch(Py_None, lib.qalora_epilogue_backward_workspace_bytes((int)T, (int)cols));
+  }
+  PLAIN(c);
+  auto data = [](const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; };
+  void *p_dy = dy->data_ptr(), *p_dz = data(dz), *p_dmul = data(dmul), *p_ws = data(ws);
+  float* p_dbias = f32(data(dbias));
+  void* st = stream();
+  if (!run("qalora_epilogue_backward", lib.qalora_epilogue_backward, act, (int)T, (int)cols, p_dy, dtype, z, mul, p_dz, p_dmul,
+           p_dbias, acc ? 1 : 0, p_ws, ws.defined() ? ws.nbytes() : 0, st))
+    return nullptr;
+  auto back = [](PyObject* o, const at::Tensor& t) { return t.defined() ? given_or(o, t) : Py_NewRef(Py_None); };
+  return tuple({back(a[6], dz), back(a[7], dmul), back(a[8], dbias)});
+FASTCALL_END
+
+// hp, params, grads, momentum, zero_grads, ws -> True
+FASTCALL(muon_step, 6)
+  constexpr Py_ssize_t kMost = QALORA_MUON_MAX_TENSORS;
+  Call c;
+  qalora_muon hp{};
+  c.read_struct(a[0], muon_type, hp);
+  c.need(PyList_CheckExact(a[1]) || PyTuple_CheckExact(a[1]));
+  PLAIN(c);
+  const Py_ssize_t count = PySequence_Fast_GET_SIZE(a[1]);
+  c.need(count >= 1 && count <= kMost);
+  float* ptr[3][kMost];
+  int32_t rows[kMost], cols[kMost];
+  PyObject** first = items(c, a[1], count);
+  for (int l = 0; c.ok && l < 3; ++l) {
+    PyObject** list = items(c, a[1 + l], count);
+    for (Py_ssize_t i = 0; c.ok && i < count; ++i) {
+      const at::Tensor* t = c.tensor(list[i], l == 0 && i == 0);
+      c.need(t && t->scalar_type() == at::kFloat && t->dim() == 2 && (l == 0 || t->sizes() == THPVariable_Unpack(first[i]).sizes()));
+      c.need(c.ok && t->size(0) <= INT32_MAX && t->size(1) <= INT32_MAX);
+      if (!c.ok) break;
+      ptr[l][i] = f32(t->data_ptr());
+      rows[i] = (int32_t)t->size(0);
+      cols[i] = (int32_t)t->size(1);
+    }
+  }
+  const bool zero = c.truth(a[4]);
+  c.on_current_device();
+  PLAIN(c);
+  const at::Tensor ws = c.scratch(a[5], a[5] == Py_None ? lib.qalora_muon_workspace_bytes((int)count, rows, cols) : 0);
+  PLAIN(c);
+  void* st = stream();
+  if (!run("qalora_muon_step", lib.qalora_muon_step, &hp, (int)count, ptr[0], ptr[1], ptr[2], rows, cols, zero ? 1 : 0,
+           ws.data_ptr(), ws.nbytes(), st))
+    return nullptr;
+  Py_RETURN_TRUE;
+FASTCALL_END
+
+// bind({entry point: address}, raise_status, Desc, AdamW, Muon)
 PyObject* bind(PyObject*, PyObject* args) {
-  PyObject *table, *raiser, *desc, *adamw;
-  if (!PyArg_ParseTuple(args, "O!OO!O!", &PyDict_Type, &table, &raiser, &PyType_Type, &desc, &PyType_Type, &adamw))
+  PyObject *table, *raiser, *desc, *adamw, *muon;
+  if (!PyArg_ParseTuple(args, "O!OO!O!O!", &PyDict_Type, &table, &raiser, &PyType_Type, &desc, &PyType_Type, &adamw,
+                        &PyType_Type, &muon))
     return nullptr;
   Library next;
 #define QALORA_BIND(name)                                                    \
@@ -612,7 +792,7 @@ PyObject* bind(PyObject*, PyObject* args) {
   }
   QALORA_ENTRIES(QALORA_BIND)
   lib = next;
-  for (auto [to, from] : {std::pair{&raise_status, raiser}, {&desc_type, desc}, {&adamw_type, adamw}}) {
+  for (auto [to, from] : {std::pair{&raise_status, raiser}, {&desc_type, desc}, {&adamw_type, adamw}, {&muon_type, muon}}) {
     Py_INCREF(from);
     Py_XSETREF(*to, from);
   }
@@ -624,7 +804,8 @@ PyObject* bind(PyObject*, PyObject* args) {
 PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr}, METHOD(quantize), METHOD(forward), METHOD(forward_keep),
                          METHOD(backward), METHOD(backward_kept), METHOD(forward_deployed), METHOD(forward_factors16),
                          METHOD(forward_shared), METHOD(backward_shared), METHOD(swiglu_forward_wide),
-                         METHOD(swiglu_backward_wide), METHOD(adamw_step), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(swiglu_backward_wide), METHOD(adamw_step), METHOD(forward_epilogue), METHOD(forward_deployed_epilogue),
+                         METHOD(epilogue_backward), METHOD(muon_step), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Native form of the binding's calls (see api.py).", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 
