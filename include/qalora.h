@@ -272,7 +272,7 @@ int qalora_forward_deployed_epilogue(const qalora_desc* desc, int tokens, const 
  * in : dy fp32 or bf16 per dy_dtype; z bf16, NULL allowed where neither act nor dmul needs it; mul bf16 or NULL
  * out: dz, dmul bf16, dbias fp32 [cols]: at least one, the others NULL; dmul only with mul; a bf16 dz may be dy itself.
  *      accumulate = 1 adds to dbias.  The slope of relu at zero is zero.
- * ws: qalora_epilogue_backward_workspace_bytes(tokens, cols) bytes, needed for dbias.  Reruns are bit-identical; may be
+ * ws: qalora_epilogue_backward_workspace_bytes(tokens, cols) bytes, needed for dbias (0: none is).  Reruns are bit-identical; may be
  * captured into a HIP graph. */
 size_t qalora_epilogue_backward_workspace_bytes(int tokens, int cols);
 int qalora_epilogue_backward(int act, int tokens, int cols, const void* dy, int dy_dtype, const void* z,

@@ -687,7 +687,8 @@ int qalora_epilogue_backward(int act, int tokens, int cols, const void* dy, int 
       misaligned(ws))
     return QALORA_EALIGN;
   if (cols % 8 != 0) return QALORA_EUNSUPPORTED;
-  if (dbias && (!ws || ws_bytes < epilogue_back_floats(tokens, cols) * sizeof(float))) return QALORA_EWORKSPACE;
+  const size_t need = dbias ? epilogue_back_floats(tokens, cols) * sizeof(float) : 0;
+  if (need > 0 && (!ws || ws_bytes < need)) return QALORA_EWORKSPACE;
   EpilogueBackArgs a{};
   a.dy = dy;
   a.z = static_cast<const uint16_t*>(z);

@@ -20,6 +20,7 @@ __device__ __forceinline__ u32x4 pack8(const float (&f)[8]) {
 }
 }  // namespace
 
+template <bool DY_BF16>
 __global__ __launch_bounds__(EB_THREADS) void epilogue_back_kernel(const EpilogueBackArgs p) {
   __shared__ float share[EB_THREADS][8 + 1];
   const int lane = threadIdx.x & (p.plan.lanes - 1), row_in = threadIdx.x / p.plan.lanes;
@@ -28,27 +29,50 @@ __global__ __launch_bounds__(EB_THREADS) void epilogue_back_kernel(const Epilogu
   const bool live = col < p.cols;
   const long r0 = (long)blockIdx.y * p.plan.rows_per, r1 = min((long)p.rows, r0 + p.plan.rows_per);
   float sum[8] = {};
-  if (live) {
+  struct Row {
+    u32x4 dy[2], z, mul;
+  };
+  auto load = [&](long r) {
+    const size_t at = (size_t)r * p.cols + col;
+    Row w{};
+    if (DY_BF16) {
+      w.dy[0] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.dy) + at);
+    } else {
+      const u32x4* src = reinterpret_cast<const u32x4*>(static_cast<const float*>(p.dy) + at);
+      w.dy[0] = src[0];
+      w.dy[1] = src[1];
+    }
+    if (p.z) w.z = *reinterpret_cast<const u32x4*>(p.z + at);
+    if (p.mul) w.mul = *reinterpret_cast<const u32x4*>(p.mul + at);
+    return w;
+  };
+  if (live && r0 + row_in < r1) {
+    Row next = load(r0 + row_in);
     for (long r = r0 + row_in; r < r1; r += at_once) {
+      const Row w = next;
+      if (r + at_once < r1) next = load(r + at_once);  // while this row is worked on
       const size_t at = (size_t)r * p.cols + col;
-      float dy[8], z[8] = {}, mul[8];
-      if (p.dy_bf16) {
-        unpack8(*reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.dy) + at), dy);
+      float dy[8], z[8], mul[8];
+      if (DY_BF16) {
+        unpack8(w.dy[0], dy);
       } else {
-        const f32x4* src = reinterpret_cast<const f32x4*>(static_cast<const float*>(p.dy) + at);
-        const f32x4 a = src[0], b = src[1];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) dy[k] = a[k], dy[4 + k] = b[k];
+        for (int k = 0; k < 8; ++k) dy[k] = __uint_as_float(w.dy[k >> 2][k & 3]);
       }
-      if (p.z) unpack8(*reinterpret_cast<const u32x4*>(p.z + at), z);
-      if (p.mul) unpack8(*reinterpret_cast<const u32x4*>(p.mul + at), mul);
+      unpack8(w.z, z);
+      unpack8(w.mul, mul);
       float dz[8], dmul[8];
+      with_act(p.act, [&](auto act) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          float value, slope;
+          act_slope<decltype(act)::value>(z[k], value, slope);
+          dmul[k] = dy[k] * value;
+          dz[k] = dy[k] * slope;
+        }
+      });
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        float value, slope;
-        act_slope(p.act, z[k], value, slope);
-        dmul[k] = dy[k] * value;
-        dz[k] = dy[k] * slope;
         if (p.mul) dz[k] *= mul[k];
         sum[k] += dz[k];
       }
@@ -56,7 +80,7 @@ __global__ __launch_bounds__(EB_THREADS) void epilogue_back_kernel(const Epilogu
       if (p.dmul) *reinterpret_cast<u32x4*>(p.dmul + at) = pack8(dmul);
     }
   }
-  if (!p.partial) return;
+  if (!p.dbias) return;
 #pragma unroll
   for (int k = 0; k < 8; ++k) share[threadIdx.x][k] = sum[k];
   __syncthreads();
@@ -64,30 +88,40 @@ __global__ __launch_bounds__(EB_THREADS) void epilogue_back_kernel(const Epilogu
     for (int r = 1; r < at_once; ++r)
 #pragma unroll
       for (int k = 0; k < 8; ++k) sum[k] += share[r * p.plan.lanes + lane][k];
-    float* o = p.partial + (size_t)blockIdx.y * p.cols + col;
+    const bool whole = gridDim.y == 1;  // the block has all rows
+    float* o = whole ? p.dbias + col : p.partial + (size_t)blockIdx.y * p.cols + col;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) o[k] = sum[k];
+    for (int k = 0; k < 8; ++k) o[k] = whole && p.accumulate ? o[k] + sum[k] : sum[k];
   }
 }
 
-// dbias = (accumulate ? dbias : 0) + the row blocks' shares, in order
+// dbias = (accumulate ? dbias : 0) + the row blocks' shares, in order: 32 columns a block, their shares dealt to eight
+// groups of threads (a thread that adds 94 of them by itself: 7 us)
 __global__ __launch_bounds__(256) void epilogue_bias_kernel(const float* __restrict__ partial, int blocks, int cols, int accumulate,
                                                             float* __restrict__ dbias) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= cols) return;
+  __shared__ float part[8][32];
+  const int e = threadIdx.x & 31, group = threadIdx.x >> 5, c = blockIdx.x * 32 + e;
+  const int per = (blocks + 7) / 8, b0 = min(blocks, group * per), b1 = min(blocks, b0 + per);
   float v = 0.0f;
-#pragma unroll 8
-  for (int b = 0; b < blocks; ++b) v += partial[(size_t)b * cols + c];
+  if (c < cols)
+#pragma unroll 16
+    for (int b = b0; b < b1; ++b) v += partial[(size_t)b * cols + c];
+  part[group][e] = v;
+  __syncthreads();
+  if (group > 0 || c >= cols) return;
+#pragma unroll
+  for (int k = 1; k < 8; ++k) v += part[k][e];
   dbias[c] = accumulate ? dbias[c] + v : v;
 }
 
 hipError_t launch_epilogue_backward(const EpilogueBackArgs& args, hipStream_t st) {
   EpilogueBackArgs a = args;
   a.plan = epilogue_back_plan(a.rows, a.cols);
-  if (!a.dbias) a.partial = nullptr;
-  epilogue_back_kernel<<<dim3(a.plan.col_blocks, a.plan.row_blocks), EB_THREADS, 0, st>>>(a);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess || !a.dbias) return e;
-  epilogue_bias_kernel<<<(a.cols + 255) / 256, 256, 0, st>>>(a.partial, a.plan.row_blocks, a.cols, a.accumulate, a.dbias);
+  const dim3 grid(a.plan.col_blocks, a.plan.row_blocks);
+  if (a.dy_bf16) epilogue_back_kernel<true><<<grid, EB_THREADS, 0, st>>>(a);
+  else epilogue_back_kernel<false><<<grid, EB_THREADS, 0, st>>>(a);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || !a.dbias || a.plan.row_blocks == 1) return e;
+  epilogue_bias_kernel<<<a.cols / 32 + (a.cols % 32 ? 1 : 0), 256, 0, st>>>(a.partial, a.plan.row_blocks, a.cols, a.accumulate, a.dbias);
   return hipGetLastError();
 }
 

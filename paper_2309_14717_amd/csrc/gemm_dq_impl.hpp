@@ -656,8 +656,9 @@ __global__ __launch_bounds__(NT, gemm_min_waves(BM, NBITS, BWD, FAST)) void gemm
     inv_n[b] = BWD ? p.n_scale[0] : (n < p.N ? p.n_scale[n] : 1.0f);
   }
   // With an epilogue the tile is staged as fp32 whatever y's type, and a thread takes eight columns of a row, the same eight
-  // of every row it comes to: its share of the bias stays in registers.
-  [[maybe_unused]] auto epilogue_with = [&](const Epilogue& epi) {
+  // of every row it comes to: its share of the bias stays in registers.  The other operands of its next rows are requested
+  // while the tile is staged, or while the rows before are finished.
+  [[maybe_unused]] auto epilogue_with = [&](const auto& epi) {
     constexpr int ROW = BN * 4 + 16;
     constexpr int kLds = (A_STAGES * BM + 2 * BN) * 64 * 2;
     constexpr int kPasses = ceil_div(BM * ROW + BM * 4, kLds);
@@ -671,8 +672,20 @@ __global__ __launch_bounds__(NT, gemm_min_waves(BM, NBITS, BWD, FAST)) void gemm
       bias[0] = reinterpret_cast<const f32x4*>(epi.bias + col)[0];
       bias[1] = reinterpret_cast<const f32x4*>(epi.bias + col)[1];
     }
-    Epilogue rest = epi;
-    rest.bias = nullptr;
+    constexpr int ROWS = RP / ROWS_AT_ONCE;  // a thread's rows of a pass
+    constexpr int AHEAD = 2;
+    static_assert(RP % ROWS_AT_ONCE == 0 && ROWS % AHEAD == 0, "whole batches of rows");
+    const bool cols_ok = col < p.N;
+    const int row0 = m0 + e_tid / CPR;
+    EpilogueOperands coming[AHEAD];
+    auto request = [&](int first) {  // the AHEAD rows from the thread's row `first` of the tile on
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        const int row = row0 + (first + k) * ROWS_AT_ONCE;
+        if (cols_ok && row < p.M) request_operands(epi, (size_t)row * p.N + col, p.out_bf16, coming[k]);
+      }
+    };
+    request(0);
     __syncthreads();  // row scales visible
 #pragma unroll
     for (int pass = 0; pass < kPasses; ++pass) {
@@ -696,21 +709,29 @@ __global__ __launch_bounds__(NT, gemm_min_waves(BM, NBITS, BWD, FAST)) void gemm
         }
       }
       __syncthreads();
-#pragma unroll 2
-      for (int rl = e_tid / CPR; rl < RP; rl += ROWS_AT_ONCE) {
-        const int row = m0 + pass * RP + rl;
-        if (row >= p.M || col >= p.N) break;
-        const size_t at = (size_t)row * p.N + col;
-        const f32x4* s = reinterpret_cast<const f32x4*>(stage + rl * ROW + ch * 32);
-        const f32x4 y0 = apply_epilogue(rest, s[0] + bias[0], at, col, p.out_bf16);
-        const f32x4 y1 = apply_epilogue(rest, s[1] + bias[1], at + 4, col + 4, p.out_bf16);
-        if (p.out_bf16) {
-          *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + at) =
-              uint4{pack_bf16x2(y0[0], y0[1]), pack_bf16x2(y0[2], y0[3]), pack_bf16x2(y1[0], y1[1]), pack_bf16x2(y1[2], y1[3])};
-        } else {
-          f32x4* o = reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at);
-          o[0] = y0;
-          o[1] = y1;
+#pragma unroll
+      for (int first = 0; first < ROWS; first += AHEAD) {
+        EpilogueOperands now[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) now[k] = coming[k];
+        if (pass + 1 < kPasses || first + AHEAD < ROWS) request(pass * ROWS + first + AHEAD);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+          const int rl = e_tid / CPR + (first + k) * ROWS_AT_ONCE, row = m0 + pass * RP + rl;
+          if (!cols_ok || row >= p.M) continue;
+          const size_t at = (size_t)row * p.N + col;
+          const f32x4* s = reinterpret_cast<const f32x4*>(stage + rl * ROW + ch * 32);
+          const f32x4 s0 = s[0] + bias[0], s1 = s[1] + bias[1];
+          float v[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
+          apply_epilogue8(epi, now[k], v, at, p.out_bf16);
+          if (p.out_bf16) {
+            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + at) =
+                uint4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+          } else {
+            f32x4* o = reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at);
+            o[0] = f32x4{v[0], v[1], v[2], v[3]};
+            o[1] = f32x4{v[4], v[5], v[6], v[7]};
+          }
         }
       }
     }
