@@ -13,11 +13,11 @@ constexpr int MUON_CHUNK = 64;       // entries of the longer side that a block 
 struct MuonTensor {
   float *p, *g, *m;      // [rows, cols]
   int rows, cols;
-  int tiles;             // 16-row tiles of the shorter side
+  int tiles;             // 32-row tiles of the shorter side
   int chunks;            // of the longer side
   float step_size;       // lr times the shape's scale
-  size_t x;              // floats from the workspace's start: X as [chunks][16 tiles][MUON_CHUNK]
-  size_t gram;           // the Gram matrix: upper 16 x 16 tiles, as MuonGram stores them
+  size_t x;              // floats from the workspace's start: X as [chunks][32 tiles][MUON_CHUNK]
+  size_t gram;           // the Gram matrix: [tiles][tiles] of 32 x 32
   size_t partial;        // each block's share of it
 };
 struct MuonTable {
@@ -26,12 +26,11 @@ struct MuonTable {
   int reduce0[MUON_MAX_TENSORS];  // first block of the launch that adds the blocks' Gram matrices
   MuonTensor t[MUON_MAX_TENSORS];
 };
-constexpr int muon_gram_tiles(int tiles) { return tiles * (tiles + 1) / 2; }
-constexpr int MUON_REDUCE_BLOCKS_PER_TILE = 2;  // (muon_reduce_kernel: 32 of a tile's 64 16-byte pieces a block)
+constexpr int MUON_REDUCE_BLOCKS_PER_TILE = 8;  // (muon_reduce_kernel: 32 of a tile's 256 16-byte pieces a block)
 
 // Blocks over X: about as many as the chip holds at once (a block first squares the Gram matrix, so more of them only
-// repeat that; 102 KB of LDS with more than 64 rows, 35 KB below).
-constexpr int muon_target_blocks(int max_tiles) { return max_tiles > 4 ? 256 : 512; }
+// repeat that; 143 KB of LDS with more than 64 rows, 55 KB below).
+constexpr int muon_target_blocks(int max_tiles) { return max_tiles > 2 ? 256 : 512; }
 
 // Fills in the table from rows[] and cols[]; returns the workspace's floats, 0 where the list is not acceptable
 // (`unsupported` says whether a matrix has both sides above MUON_MAX_SHORT, rather than a bad argument).
@@ -48,7 +47,7 @@ inline size_t muon_table(int n, const int32_t* rows, const int32_t* cols, MuonTa
     t.cols = cols[i];
     const int shorter = rows[i] < cols[i] ? rows[i] : cols[i], longer = rows[i] < cols[i] ? cols[i] : rows[i];
     if (shorter > MUON_MAX_SHORT) unsupported = true;
-    t.tiles = (shorter + 15) / 16;
+    t.tiles = (shorter + 31) / 32;
     t.chunks = longer / MUON_CHUNK + (longer % MUON_CHUNK ? 1 : 0);
     if (t.tiles > table.max_tiles) table.max_tiles = t.tiles;
     chunks += t.chunks;
@@ -61,13 +60,13 @@ inline size_t muon_table(int n, const int32_t* rows, const int32_t* cols, MuonTa
   for (int i = 0; i < n; ++i) {
     MuonTensor& t = table.t[i];
     const int blocks = (t.chunks + table.per_block - 1) / table.per_block;
-    const size_t gram = (size_t)muon_gram_tiles(t.tiles) * 256;
+    const size_t gram = (size_t)t.tiles * t.tiles * 1024;
     table.block0[i] = table.blocks;
     table.reduce0[i] = table.reduce_blocks;
     table.blocks += blocks;
-    table.reduce_blocks += muon_gram_tiles(t.tiles) * MUON_REDUCE_BLOCKS_PER_TILE;
+    table.reduce_blocks += t.tiles * t.tiles * MUON_REDUCE_BLOCKS_PER_TILE;
     t.x = floats;
-    floats += (size_t)t.chunks * t.tiles * 16 * MUON_CHUNK;
+    floats += (size_t)t.chunks * t.tiles * 32 * MUON_CHUNK;
     t.gram = floats;
     floats += gram;
     t.partial = floats;

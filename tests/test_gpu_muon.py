@@ -227,3 +227,17 @@ def test_refusals(gpu_api):
     with pytest.raises(ValueError):
         gpu_api.muon_step(hp, [], [], [])
     assert not ok[0].any()
+
+
+@pytest.mark.parametrize("size", [1e-15, 1e-8, 1.0, 1e8, 1e15])
+def test_gradients_of_any_size(gpu_api, size):
+    """The direction does not depend on the gradients' size (eps far below them)."""
+    rng = np.random.default_rng(14)
+    shapes = [(16, 300), (100, 700), (513, 40)]
+    g = [gradient(rng, *s) * np.float32(size) for s in shapes]
+    hp = gpu_api.Muon(lr=1.0, momentum=0.0, eps=1e-20, nesterov=False, scale_mode=0)
+    dp, dg, dm = up([np.zeros(s, np.float32) for s in shapes]), up(g), up([np.zeros(s, np.float32) for s in shapes])
+    gpu_api.muon_step(hp, dp, dg, dm)
+    for i in range(len(shapes)):
+        ref, bound = orthogonal(g[i].astype(np.float64), hp.steps, float(hp.eps))
+        assert np.sqrt(((-dp[i].cpu().numpy().astype(np.float64) - ref) ** 2).sum()) <= bound

@@ -60,11 +60,11 @@ def test_table_covers_every_matrix_once(plan):
         end = block = reduce = 0
         for (rows, cols), (tiles, chunks, block0, reduce0, x, gram, partial) in zip(shapes, ts):
             short, long = min(rows, cols), max(rows, cols)
-            assert 16 * (tiles - 1) < short <= 16 * tiles <= 16 * max_tiles and 64 * (chunks - 1) < long <= 64 * chunks
-            slices, g = -(-chunks // per_block), tiles * (tiles + 1) // 2 * 256
+            assert 32 * (tiles - 1) < short <= 32 * tiles <= 32 * max_tiles and 64 * (chunks - 1) < long <= 64 * chunks
+            slices, g = -(-chunks // per_block), tiles * tiles * 1024
             assert (block0, reduce0, x) == (block, reduce, end)           # regions follow each other without a gap
-            assert gram == x + chunks * tiles * 16 * 64 and partial == gram + g
-            end, block, reduce = partial + slices * g, block + slices, reduce + tiles * (tiles + 1)
+            assert gram == x + chunks * tiles * 32 * 64 and partial == gram + g
+            end, block, reduce = partial + slices * g, block + slices, reduce + 8 * tiles * tiles
             assert x % 4 == gram % 4 == partial % 4 == 0                  # 16-byte accesses
         assert (floats, blocks, reduce_blocks) == (end, block, reduce) and blocks < 2 ** 31
 
