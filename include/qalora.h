@@ -421,10 +421,10 @@ int qalora_adamw_step(const qalora_adamw* hp, int step, int n_tensors, float* co
  * params, grads, momentum: HOST arrays of n_tensors DEVICE pointers (fp32, row-major, 16-byte aligned, no two the same);
  * params and momentum are updated in place; grads are read, and set to zero afterwards if zero_grads != 0.
  * rows, cols: HOST arrays.  The shorter side is at most QALORA_MUON_MAX_SHORT (the rank of an adapter;
- * QALORA_EUNSUPPORTED otherwise); the longer one is any.  eps > 0; a matrix of zeros gets the update zero.
+ * QALORA_EUNSUPPORTED otherwise), the longer one at most 2^27.  eps > 0; a matrix of zeros gets the update zero.
  * A matrix with an infinity or a NaN in u becomes NaN, the others do not see it.
- * ws: qalora_muon_workspace_bytes(n_tensors, rows, cols) bytes (0 for a list that is not acceptable), about what the matrices
- * take themselves.  fp32 arithmetic, sums in a fixed order: a step is bit-reproducible.  Errors of the sums, about 2^-24 of
+ * ws: qalora_muon_workspace_bytes(n_tensors, rows, cols) bytes (0 for a list that is not acceptable): what the matrices take
+ * themselves with every shorter side padded to 32, 64 or 128 (the same for all), and up to 21 MB.  fp32 arithmetic, sums in a fixed order: a step is bit-reproducible.  Errors of the sums, about 2^-24 of
  * |u|_F, grow with the smallest singular values, by up to a^steps.  May be captured into a HIP graph, after an eager call
  * of as many steps. */
 #define QALORA_MUON_MAX_TENSORS 32

@@ -8,27 +8,39 @@
 //        a t + b t^3 + c t^5 and its iterates bring them all near one, while the singular vectors stay
 //   p  = p (1 - lr wd) - lr scale X
 //
-// G is r x r: it fits a compute unit, X does not.  So a step of the iteration is one pass over X: a block takes G, forms
-// P = a I + b G + c G^2 in LDS (r^3 operations, repeated by every block, against r^2 per column of X), replaces its
+// G is r x r: it fits a compute unit, X mostly does not.  So a step of the iteration is one pass over X: a block takes G, forms
+// P = a I + b G + c G^2 (r^3 operations, repeated by every block, against r^2 per column of X), replaces its
 // columns of X by P X and adds the new columns' products to its own share of the next G; a small launch adds the shares in
 // block order (no atomics: a step is bit-reproducible).  X0's norm is the root of the first G's trace and goes into the first
-// pass, so the norm takes no pass of its own.
+// pass, so the norm takes no pass of its own.  Small matrices (a block's work of a few microseconds a pass) take one launch, a block
+// each: the launches of a step are eleven with five passes.
 //
 // (G alone could carry the whole iteration: P is a polynomial in the first G.  But an error of 2^-24 in that G then meets
 // the smallest singular values with the full gain a^steps, 1.5 % of the result for the coefficients in use.  G made
 // anew from X in every pass keeps it at 2^-24 times the gain.)
 //
-// Products.  X, G and P are fp32; for the matrix cores a value is split in two fp16, hi = fp16(S v) and lo = fp16(2^12 (S v - hi)),
-// S a power of two that keeps S v below 2^15.  Three products, hi hi + 2^-12 (hi lo + lo hi), miss 2^-24 of the operands, as
-// rounding them to fp32 does, and take a fifth of the time of the fp32 instruction (which has a sixteenth of the fp16 rate).
-// (The scale of lo keeps it away from fp16's subnormals, and makes up for hi where that is one: S may be far from tight.  It
-// comes from bounds: |G_ij| <= trace G, |X_ij| <= |X|_F = sqrt(trace G), |P_ij| <= |a| + |b| trace G + |c| (trace G)^2, and of
-// P X their product.)
+// Products.  X, G and P are fp32; for the matrix cores a value v is split in two fp16, hi = fp16(S v) and lo = fp16(S v - hi), S a
+// power of two that keeps S v below 2^15.  Three products, hi hi + hi lo + lo hi, miss 2^-24 of the operands, as rounding them
+// to fp32 does, wherever S v is above 1/2 or so (below, lo is an fp16 subnormal: 2^-25 in all, however small S v), and take a fifth
+// of the time of the fp32 instruction (which has a sixteenth of the fp16 rate).  S comes from bounds: |G_ij| <= trace G,
+// |X_ij| <= |X|_F = sqrt(trace G), |P_ij| <= |P|_F, and of P X their product; the values of most weight are then 2^3 and more,
+// P X's 2^-2.
 //
-// Layout.  v_mfma_f32_32x32x16_f16: X in LDS as [rows i][64 columns n] planes of hi and lo.  P X is computed transposed (A operand: X
-// read transposed, ds_read_b64_tr_b16; B operand: rows of P, by its symmetry), so a lane holds four neighbouring n of a
-// row i and writes them back 8 bytes at a time; X X^T reads rows of the same planes.  In memory X is kept as the lanes hold
-// it ([32 x 32 tile][register quad][lane] of 16 bytes), so a pass reads and writes it in whole kilobytes.
+// Layout.  A wavefront owns 32 columns of X at a time and needs neither LDS nor other wavefronts for them.  The 32 x 32 result of
+// v_mfma_f32_32x32x16_f16 leaves in lane l the column l % 32 and, of quad q (registers 4 q ..), the rows 8 q + 4 (l / 32) + 0..3.  As an
+// operand a lane supplies eight values of the contraction index for its row (or column) l % 32, and which index is which is
+// free as long as both operands agree: with quads 2 s and 2 s + 1 as the eight values of slice s, a result IS an operand
+// whose row is its column.  So X is kept (in memory too: [32 columns][32-row tile][quad][lane], 16 bytes a lane) as P X leaves the
+// matrix cores, and goes back into them as it is; P, symmetric, likewise; and for X X^T, whose contraction runs over the columns,
+// the tile is turned by a product with the unit matrix, exact for hi and lo each.
+//
+// Measured, five passes: the seven adapters of a 4096 / 11008 layer at rank 64, 44 MB of p, g, m and X: 97 us (fp32 products of the
+// recipe alone 18 us at the card's rate, the bytes that cannot be spared 11 us): 17 us of momentum and first G, 5 x 4.8 us adding
+// shares, 5 x 12.6 us passes, of which 2 to 3 us are a launch, as much again P, and the rest one or two chunks a wavefront.  Rank 128
+// at 8192 / 22016, 178 MB: 282 us, of 69, 5 x 5.4 and 4 x 37 + 51 us: X, 45 MB, goes through memory in every pass at 2.4 TB/s,
+// beside 170 matrix instructions and 600 others a chunk of one wavefront a SIMD (its sums and operands take more than
+// half of the registers).  Two adapters of 1024 at rank 16: 41 us, one launch, bound by the instructions of its two compute units.
+// Operands of P and X through LDS and 64 columns a block instead of 32 a wavefront: 107, 266 and 57 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -39,13 +51,6 @@ namespace qalora {
 
 namespace {
 
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-
-constexpr int XLD = MUON_CHUNK + 8;  // halves between rows of a chunk's plane: 16-byte reads of 32 rows meet all banks
-constexpr float kLoScale = 4096.0f;
-
 // A power of two that brings magnitudes up to `bound` below 2^15.
 __device__ __forceinline__ float scale_below(float bound) {
   const int e = (int)((__float_as_uint(bound) >> 23) & 255u) - 127;
@@ -55,69 +60,70 @@ __device__ __forceinline__ float inverse_power(float s) { return __uint_as_float
 // What sqrt(trace) may miss: squares below the smallest fp32 that were lost in the sums.
 constexpr float kLostNorm = 0x1p-47f;
 
-// hi and lo of a value.  (The value is pinned to its fp32 rounding: where it is a product, the compiler rounds that once
-// more, to fp16, for the hi that is stored and otherwise for the hi that lo is taken from, and near a tie the two differ.)
-__device__ __forceinline__ void split(float v, _Float16& h, _Float16& l) {
-  asm volatile("" : "+v"(v));
-  h = (_Float16)v;
-  l = (_Float16)((v - (float)h) * kLoScale);
-}
-// Four neighbouring values into the planes (lo `lo_at` halves behind hi).
-__device__ __forceinline__ void put4(_Float16* hi, int lo_at, const f32x4& v) {
-  f16x4 h, l;
+// hi and lo of the operand of one slice: two quads.
+struct Operand {
+  f16x8 hi, lo;
+};
+// Four instructions for two values: two at a time to fp16, and the rest by v_fma_mix_f32, which takes hi as it is (with a minus
+// one that the compiler does not see through; with a constant it makes a conversion and a difference of it).  The values are
+// pinned to their fp32 rounding: where one is a product, the compiler rounds that once more, to fp16, for the hi that is
+// kept and otherwise for the hi that lo is taken from, and near a tie the two differ.
+__device__ __forceinline__ Operand split(const f32x4& q0, const f32x4& q1) {
+  float minus_one = -1.0f;
+  asm("" : "+s"(minus_one));
+  f16x2 hi[4], lo[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    _Float16 a, b;
-    split(v[e], a, b);
-    h[e] = a;
-    l[e] = b;
+  for (int k = 0; k < 4; ++k) {
+    f32x2 v = k < 2 ? f32x2{q0[2 * k], q0[2 * k + 1]} : f32x2{q1[2 * k - 4], q1[2 * k - 3]};
+    asm volatile("" : "+v"(v));
+    hi[k] = __builtin_convertvector(v, f16x2);
+    const f32x2 rest = {__builtin_fmaf((float)hi[k][0], minus_one, v[0]), __builtin_fmaf((float)hi[k][1], minus_one, v[1])};
+    lo[k] = __builtin_convertvector(rest, f16x2);
   }
-  *reinterpret_cast<f16x4*>(hi) = h;
-  *reinterpret_cast<f16x4*>(hi + lo_at) = l;
+  return Operand{__builtin_shufflevector(__builtin_shufflevector(hi[0], hi[1], 0, 1, 2, 3), __builtin_shufflevector(hi[2], hi[3], 0, 1, 2, 3), 0, 1, 2, 3, 4, 5, 6, 7),
+                 __builtin_shufflevector(__builtin_shufflevector(lo[0], lo[1], 0, 1, 2, 3), __builtin_shufflevector(lo[2], lo[3], 0, 1, 2, 3), 0, 1, 2, 3, 4, 5, 6, 7)};
 }
-__device__ __forceinline__ void put1(_Float16* hi, int lo_at, float v) {
-  _Float16 h, l;
-  split(v, h, l);
-  *hi = h;
-  hi[lo_at] = l;
+__device__ __forceinline__ f16x8 to_half(const f32x16& v, int first) {
+  f16x2 p[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) p[k] = __builtin_convertvector((f32x2{v[first + 2 * k], v[first + 2 * k + 1]}), f16x2);
+  return __builtin_shufflevector(__builtin_shufflevector(p[0], p[1], 0, 1, 2, 3), __builtin_shufflevector(p[2], p[3], 0, 1, 2, 3), 0, 1, 2, 3, 4, 5, 6, 7);
 }
-__device__ __forceinline__ f16x8 read8(const _Float16* p) { return *reinterpret_cast<const f16x8*>(p); }
-// Eight rows of one column per lane: the operand whose 32 columns and 16 rows start at `tile`
-__device__ __forceinline__ f16x8 read_columns(const _Float16* tile, int lane) {
-  const int i = lane & 15, row = 8 * (lane >> 5) + (i >> 2), col = 16 * ((lane >> 4) & 1) + 4 * (i & 3);
-  const _Float16* p = tile + row * XLD + col;
-  typedef __attribute__((address_space(3))) s16x4* lds_ptr;
-  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p));
-  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + 4 * XLD));
-  return __builtin_bit_cast(f16x8, (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+__device__ __forceinline__ void add(f32x16& acc, const Operand& a, const Operand& b) {
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.hi, b.hi, acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.hi, b.lo, acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.lo, b.hi, acc, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 zero16() {
+  f32x16 z;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = 0.0f;
+  return z;
+}
+__device__ __forceinline__ f32x4 quad_of(const f32x16& v, int q) { return f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]}; }
+
+// The unit matrix as an operand: slice s of a tile.
+__device__ __forceinline__ f16x8 unit_slice(int s, int lane) {
+  f16x8 u;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) u[k] = (_Float16)(16 * s + (k >> 2) * 8 + 4 * (lane >> 5) + (k & 3) == (lane & 31) ? 1.0f : 0.0f);
+  return u;
+}
+// The operand tile `in` (its two slices) with rows and contraction index exchanged.
+__device__ __forceinline__ void turn(const Operand (&in)[2], const f16x8 (&unit)[2], Operand (&out)[2]) {
+  f32x16 hi = zero16(), lo = zero16();
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    hi = __builtin_amdgcn_mfma_f32_32x32x16_f16(in[s].hi, unit[s], hi, 0, 0, 0);
+    lo = __builtin_amdgcn_mfma_f32_32x32x16_f16(in[s].lo, unit[s], lo, 0, 0, 0);
+  }
+#pragma unroll
+  for (int s = 0; s < 2; ++s) out[s] = Operand{to_half(hi, 8 * s), to_half(lo, 8 * s)};
 }
 
-// A 32 x 32 tile of a product: `main` of the hi pieces, `cross` of hi and lo.  Register r of a lane is element
-// (8 (r / 4) + 4 (lane / 32) + r % 4, lane % 32).
-struct Tile {
-  f32x16 main, cross;
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int r = 0; r < 16; ++r) main[r] = cross[r] = 0.0f;
-  }
-  __device__ __forceinline__ void add(const f16x8& a, const f16x8& a_lo, const f16x8& b, const f16x8& b_lo) {
-    main = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, main, 0, 0, 0);
-    cross = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b_lo, cross, 0, 0, 0);
-    cross = __builtin_amdgcn_mfma_f32_32x32x16_f16(a_lo, b, cross, 0, 0, 0);
-  }
-  __device__ __forceinline__ f32x4 quad(int g, float scale) const {
-    f32x4 v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(cross[4 * g + e], 1.0f / kLoScale, main[4 * g + e]) * scale;
-    return v;
-  }
-};
-// += rows of tile i times rows of tile j over 16 `groups` columns; both at the lane's first operand
-__device__ __forceinline__ void add_rows(Tile& t, const _Float16* rows_i, const _Float16* rows_j, int lo_at, int groups) {
-#pragma unroll 2
-  for (int s = 0; s < groups; ++s)
-    t.add(read8(rows_i + 16 * s), read8(rows_i + 16 * s + lo_at), read8(rows_j + 16 * s), read8(rows_j + 16 * s + lo_at));
-}
+// The upper tiles of a symmetric RT x RT matrix of tiles in the order (0,0), (0,1), (1,1), (0,2), ...
+constexpr int muon_upper(int tiles) { return muon_upper_tiles(tiles); }
+constexpr int upper_at(int a, int b) { return b * (b + 1) / 2 + a; }
 
 // The tensor whose blocks the launch's block lies in.  (All starts are compared at once: a search that reads one after
 // the other waits for each, 0.15 us a tensor.)
@@ -127,189 +133,476 @@ __device__ __forceinline__ int muon_find(const int (&first)[MUON_MAX_TENSORS]) {
   for (int i = 1; i < MUON_MAX_TENSORS; ++i) ti += (int)blockIdx.x >= first[i] ? 1 : 0;
   return ti;
 }
-struct Where {
-  const MuonTensor* t;
-  int c0, c1;  // chunks
-  int slice;
-};
-__device__ __forceinline__ Where muon_where(const MuonTable& table) {
-  const int ti = muon_find(table.block0);
-  const MuonTensor& t = table.t[ti];
-  Where w{&t, 0, 0, (int)blockIdx.x - table.block0[ti]};
-  w.c0 = w.slice * table.per_block;
-  w.c1 = min(t.chunks, w.c0 + table.per_block);
-  return w;
-}
 
-// A thread's share of a chunk of a [rows, cols] matrix: W neighbours in memory (4 where rows of it are whole 16-byte pieces,
-// else 1) at a time, f(k, element, i, n) for the k-th of them, (i, n) the first one's place in X's chunk; the others follow
-// along n where the matrix is wide, along i where it is tall.  The count is a constant, so that all loads of a share are in
-// flight together.
-template <int RT, int NT, int W, typename Fn>
-__device__ __forceinline__ void each_piece(const MuonTensor& t, int chunk, Fn&& f) {
-  const int n0 = chunk * MUON_CHUNK;
-  const bool wide = t.rows <= t.cols;
-  const int per_row = wide ? MUON_CHUNK / W : t.cols / W, rows = wide ? t.rows : min(MUON_CHUNK, t.rows - n0);
-#pragma unroll
-  for (int k = 0; k < 32 * RT * MUON_CHUNK / (NT * W); ++k) {
-    const int e = threadIdx.x + NT * k;
-    const int r = wide ? e / (MUON_CHUNK / W) : e / per_row, c = W * (e - r * per_row);
-    if (r >= rows || (wide && n0 + c >= t.cols)) continue;
-    f(k, wide ? (size_t)r * t.cols + n0 + c : (size_t)(n0 + r) * t.cols + c, wide ? r : c, wide ? c : r);
-  }
-}
-template <int W>
-struct Piece {
-  float v[W];
-};
-template <int W>
-__device__ __forceinline__ Piece<W> load_piece(const float* p) {
-  Piece<W> r;
-  if constexpr (W == 4) {
-    const f32x4 v = *reinterpret_cast<const f32x4*>(p);
-    for (int e = 0; e < 4; ++e) r.v[e] = v[e];
-  } else {
-    r.v[0] = *p;
-  }
-  return r;
-}
-template <int W>
-__device__ __forceinline__ void store_piece(float* p, const Piece<W>& r) {
-  if constexpr (W == 4) *reinterpret_cast<f32x4*>(p) = f32x4{r.v[0], r.v[1], r.v[2], r.v[3]};
-  else *p = r.v[0];
-}
-
-// Where element (i, n) of a chunk is kept in memory (floats; n's neighbours in a run of four follow).
-__device__ __forceinline__ int kept_at(int i, int n) {
-  return (((i >> 5) * 2 + (n >> 5)) * 4 + ((n & 31) >> 3)) * 256 + ((i & 31) + 32 * ((n >> 2) & 1)) * 4 + (n & 3);
-}
-
-constexpr int muon_waves(int rt) { return 2 * rt; }  // a wavefront per 32 x 32 tile of a chunk
-constexpr int muon_pld(int rt) { return 32 * rt + 8; }  // halves between rows of a plane of G and P
-constexpr int muon_x_halves(int rt) { return 32 * rt * XLD; }  // of a plane
-constexpr int muon_p_halves(int rt) { return 32 * rt * muon_pld(rt); }
-constexpr size_t muon_pass_lds(int rt) { return 2 * (size_t)(2 * muon_x_halves(rt) + muon_p_halves(rt)) * 2; }
-
-// A block's share of G: its wavefronts' tiles (a, b), `wave + NW q` of a tiles x tiles grid.
+// Reads or writes the lane's elements of 32 columns of X, from column n0 on, in a [rows, cols] matrix.
+// Wide (rows <= cols): 32 lanes take 128 bytes of a row.  A buffer per row (its start is the same for the wavefront) and no
+// branches: what lies outside the matrix is aimed past the buffer, where loads give zero and stores nothing.  (With a branch around
+// each load the compiler waits for them a few at a time.)
+// Tall (an adapter's A): the 32 columns of X are one run of memory; it goes through the wavefront's room in LDS, as
+// [n][MUON_TURN_LD].  (Lanes reading their elements from as many rows took 21 us of the first launch over muon_layer's matrices.)
+constexpr int muon_turn_ld(int rt) { return 32 * rt + 4; }
+constexpr size_t muon_turn_floats(int rt) { return (size_t)32 * muon_turn_ld(rt); }
 template <int RT>
-struct Gram {
-  static constexpr int NW = muon_waves(RT), Q = RT * RT / NW;
-  int at_a[Q], at_b[Q], tiles, wave;
-  __device__ __forceinline__ Gram(int tiles_, int wave_, int lane, int ld) : tiles(tiles_), wave(wave_) {
+struct Elements {
+  static constexpr int LD = muon_turn_ld(RT);
+  bool wide, column;
+  int rows, cols, hi4, lane, run;
+  size_t base;
+  uint32_t away, reciprocal;
+  float* room;
+  __device__ __forceinline__ Elements(const MuonTensor& t, int n0, int lane_, float* room_)
+      : wide(t.rows <= t.cols), rows(t.rows), cols(t.cols), hi4(4 * (lane_ >> 5)), lane(lane_), room(room_) {
+    column = n0 + (lane & 31) < max(rows, cols);
+    base = wide ? (size_t)n0 : (size_t)n0 * cols;
+    away = column ? 4u * ((uint32_t)hi4 * (uint32_t)cols + (lane & 31)) : 0xfffffffcu;
+    run = wide ? 0 : min(32, rows - n0) * cols;                       // of a tall matrix
+    reciprocal = wide ? 0 : ((1u << 20) + cols - 1) / (uint32_t)cols;  // e / cols = e * this >> 20 for e < 4096, cols <= 128
+  }
+  // The buffers of rows, for one use.  (Opaque: the compiler would work out all rows' starts and sizes ahead of the loop over
+  // chunks and for the next use, and keep them in the lanes of vector registers: 1500 moves a chunk at 128 rows.)
+  struct Rows {
+    float* start;
+    int rows, cols;
+    __device__ __forceinline__ Rows(const Elements& e, const float* p) : start(const_cast<float*>(p) + e.base), rows(e.rows), cols(e.cols) {
+      asm volatile("" : "+s"(start), "+s"(rows), "+s"(cols));
+    }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t operator[](int k) const {
+      const uint32_t bytes = k + 4 < rows ? 0xfffffffcu : (k < rows ? 16u * cols : 0u);  // (row k + 4 is the upper lanes')
+      return __builtin_amdgcn_make_buffer_rsrc(start + (size_t)k * cols, 0, (int)bytes, 0x00020000);
+    }
+  };
+  // element lane + 64 k of the run, in LDS
+  __device__ __forceinline__ float* turned(int k) const {
+    int at = lane;
+    asm volatile("" : "+v"(at));  // (else all of them are worked out once, and their registers held throughout)
+    const uint32_t e = at + 64 * k, n = e * reciprocal >> 20;
+    return room + n * LD + (e - n * cols);
+  }
+  __device__ __forceinline__ int mine() const {  // what of the run lies from the lane on
+    int left = run - lane;
+    asm volatile("" : "+v"(left));
+    return left;
+  }
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t run_buffer(const float* p) const {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(p) + base, 0, 4 * run, 0x00020000);
+  }
+  static __device__ __forceinline__ void handed_over() {  // between the lanes of the wavefront, through LDS
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  // In two parts, so that other work can lie between: the loads, and (of a tall matrix) each element to its lane.
+  __device__ __forceinline__ void request(const float* p, f32x4 (&v)[4 * RT]) const {
+    if (wide) {
+      const Rows row(*this, p);
 #pragma unroll
-    for (int q = 0; q < Q; ++q) {
-      const int id = wave + NW * q, a = id / tiles, b = id - a * tiles;
-      at_a[q] = (32 * a + (lane & 31)) * ld + 8 * (lane >> 5);
-      at_b[q] = (32 * b + (lane & 31)) * ld + 8 * (lane >> 5);
+      for (int q = 0; q < 4 * RT; ++q) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[q][e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(row[8 * q + e], (int)away, 0, 0));
+        __builtin_amdgcn_sched_barrier(0);  // (else the buffers of all rows are made first, and scalar registers run out)
+      }
+      return;
+    }
+    const __amdgpu_buffer_rsrc_t rs = run_buffer(p);
+#pragma unroll
+    for (int k = 0; k < 16 * RT; ++k) v[k >> 2][k & 3] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, 4 * (lane + 64 * k), 0, 0));
+  }
+  __device__ __forceinline__ void settle(f32x4 (&v)[4 * RT]) const {
+    if (wide) return;
+    handed_over();
+    const int left = mine();
+#pragma unroll
+    for (int k = 0; k < 16 * RT; ++k)
+      if (64 * k < left) *turned(k) = v[k >> 2][k & 3];
+    handed_over();
+    int limit = column ? cols - hi4 : 0;
+    asm volatile("" : "+v"(limit));
+#pragma unroll
+    for (int q = 0; q < 4 * RT; ++q) {
+      const f32x4 r = *reinterpret_cast<const f32x4*>(room + (lane & 31) * LD + 8 * q + hi4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[q][e] = 8 * q + e < limit ? r[e] : 0.0f;
     }
   }
-  __device__ __forceinline__ bool live(int q) const { return wave + NW * q < tiles * tiles; }
+  __device__ __forceinline__ void store(float* p, const f32x4 (&v)[4 * RT]) const {
+    if (wide) {
+      const Rows row(*this, p);
+#pragma unroll
+      for (int q = 0; q < 4 * RT; ++q) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[q][e]), row[8 * q + e], (int)away, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      return;
+    }
+    handed_over();
+#pragma unroll
+    for (int q = 0; q < 4 * RT; ++q) *reinterpret_cast<f32x4*>(room + (lane & 31) * LD + 8 * q + hi4) = v[q];
+    handed_over();
+    const __amdgpu_buffer_rsrc_t rs = run_buffer(p);
+    const int left = mine();
+    float r[16 * RT];
+#pragma unroll
+    for (int k = 0; k < 16 * RT; ++k) r[k] = 64 * k < left ? *turned(k) : 0.0f;
+#pragma unroll
+    for (int k = 0; k < 16 * RT; ++k) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(r[k]), rs, 4 * (lane + 64 * k), 0, 0);
+  }
 };
+
+constexpr int muon_waves(int rt) { return muon_waves_of(rt); }  // of a block: 512 registers each, or 256
+
+// The wavefronts' G tiles (upper ones, in results' layout) added in order; the sum is the first wavefront's.
+template <int RT>
+__device__ __forceinline__ void add_shares(f32x16 (&g)[muon_upper(RT)], f32x4* lds, int wave, int lane) {
+  constexpr int NW = muon_waves(RT), U = muon_upper(RT);
+#pragma unroll
+  for (int half = NW / 2; half >= 1; half /= 2) {  // the upper half of the wavefronts to the lower one
+    __syncthreads();
+    if (wave >= half && wave < 2 * half)
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) lds[(((wave - half) * U + u) * 4 + q) * 64 + lane] = quad_of(g[u], q);
+    __syncthreads();
+    if (wave < half)
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 v = lds[((wave * U + u) * 4 + q) * 64 + lane];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) g[u][4 * q + e] += v[e];
+        }
+  }
+}
+template <int RT>
+__device__ __forceinline__ void store_share(f32x16 (&g)[muon_upper(RT)], f32x4* lds, f32x4* out, int wave, int lane) {
+  add_shares<RT>(g, lds, wave, lane);
+  if (wave == 0)
+#pragma unroll
+    for (int u = 0; u < muon_upper(RT); ++u)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) out[(u * 4 + q) * 64 + lane] = quad_of(g[u], q);
+}
+// Quad q of G's tile (a, b) and, off the diagonal, its mirror image: element (8 q + 4 (lane / 32) + k, lane % 32) at its place.
+template <int RT>
+__device__ __forceinline__ void put_gram(float* gram, int a, int b, int q, int lane, const f32x4& v) {
+  *reinterpret_cast<f32x4*>(gram + (a * RT + b) * 1024 + (q * 64 + lane) * 4) = v;
+  if (a == b) return;
+  const int col = lane & 31;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int row = 8 * q + 4 * (lane >> 5) + k;
+    gram[(b * RT + a) * 1024 + ((col >> 3) * 64 + row + 32 * ((col >> 2) & 1)) * 4 + (col & 3)] = v[k];
+  }
+}
+constexpr size_t muon_share_lds(int rt) { return (size_t)muon_waves(rt) / 2 * muon_upper(rt) * 4096; }
+constexpr size_t muon_p_lds(int rt) { return (size_t)rt * rt * 4096; }
+constexpr size_t muon_turn_lds(int rt) { return muon_waves(rt) * muon_turn_floats(rt) * 4; }
+constexpr size_t muon_start_lds(int rt) { return std::max(muon_share_lds(rt), muon_turn_lds(rt)); }
+constexpr size_t muon_alone_lds(int rt) { return 2 * muon_p_lds(rt) + muon_start_lds(rt); }
+constexpr size_t muon_pass_lds(int rt, bool last) { return last ? muon_p_lds(rt) + muon_turn_lds(rt) : std::max(muon_share_lds(rt), muon_p_lds(rt)); }
+
+// G's tiles from 32 columns of X as operands, rows of X as rows: g[(a, b)] += x_a x_b^T.
+template <int RT>
+__device__ __forceinline__ void add_gram(f32x16 (&g)[muon_upper(RT)], const Operand (&x)[RT][2]) {
+#pragma unroll
+  for (int b = 0; b < RT; ++b)
+#pragma unroll
+    for (int a = 0; a <= b; ++a)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) add(g[upper_at(a, b)], x[a][s], x[b][s]);
+}
+
+// u = the momentum's step on 32 columns, in results' layout; returns the largest magnitude in the wavefront.
+template <int RT>
+__device__ __forceinline__ float momentum_step(const MuonTensor& t, const MuonHyper& h, int n0, int lane, float* room, f32x4 (&u)[4 * RT]) {
+  const Elements<RT> at(t, n0, lane, room);
+  f32x4 m[4 * RT];
+  at.request(t.g, u);
+  at.request(t.m, m);
+  at.settle(u);
+  at.settle(m);
+  float most = 0.0f;
+#pragma unroll
+  for (int q = 0; q < 4 * RT; ++q)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      m[q][e] = __builtin_fmaf(h.momentum, m[q][e], u[q][e]);
+      u[q][e] = h.nesterov ? __builtin_fmaf(h.momentum, m[q][e], u[q][e]) : m[q][e];
+      most = fmaxf(most, fabsf(u[q][e]));
+    }
+  __builtin_amdgcn_sched_barrier(0);  // (stores between the waits for loads would be waited for, too)
+  at.store(t.m, m);
+  if (h.zero_grads) {
+    f32x4 zero[4 * RT];
+#pragma unroll
+    for (int q = 0; q < 4 * RT; ++q) zero[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    at.store(t.g, zero);
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, 64));
+  return most;
+}
+
+// The scales of a pass and the norm that comes off X in the first one.
+struct Scales {
+  float x_norm, g, x;  // x: of X once its norm is off
+  float p, y;          // of P and of P X (once P is there)
+  float trace, x_bound;
+  __device__ __forceinline__ Scales(float trace_, float eps, bool first) {
+    x_norm = first ? 1.0f / (__fsqrt_rn(trace_) + eps) : 1.0f;
+    x_bound = (__fsqrt_rn(trace_) + kLostNorm) * x_norm;
+    trace = trace_ * x_norm * x_norm;
+    g = scale_below(trace);
+    x = scale_below(x_bound);
+  }
+};
+
+// Operands in LDS: [tile][slice][hi, lo][lane] of 16 bytes.
+__device__ __forceinline__ void put_operands(f32x4* lds, int tile, int lane, const f32x4 (&q)[4], float scale) {
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const Operand o = split(q[2 * s] * scale, q[2 * s + 1] * scale);
+    lds[(2 * tile + s) * 128 + lane] = __builtin_bit_cast(f32x4, o.hi);
+    lds[(2 * tile + s) * 128 + 64 + lane] = __builtin_bit_cast(f32x4, o.lo);
+  }
+}
+__device__ __forceinline__ Operand operand_at(const f32x4* lds, int tile, int s, int lane) {
+  const f32x4* at = lds + (2 * tile + s) * 128 + lane;
+  return Operand{__builtin_bit_cast(f16x8, at[0]), __builtin_bit_cast(f16x8, at[64])};
+}
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
+  return v;
+}
+
+// The chunks of a wavefront: every muon_waves-th of its block's.
+template <int RT>
+struct Columns {
+  const MuonTensor& t;
+  f32x4* x;     // the lane's place in X
+  int first, end;
+  int wave, lane;
+  float* room;  // the wavefront's, for tall matrices
+  __device__ __forceinline__ Columns(const MuonTensor& t_, float* ws, int begin, int end_, float* rooms)
+      : t(t_), end(end_), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63) {
+    first = begin + wave;
+    x = reinterpret_cast<f32x4*>(ws + t.x) + lane;
+    room = rooms + wave * muon_turn_floats(RT);
+  }
+  __device__ __forceinline__ f32x4* at(int c) const { return x + (size_t)c * RT * 256; }
+  __device__ __forceinline__ void request(int c, f32x4 (&coming)[4 * RT]) const {
+    if (c < end)
+#pragma unroll
+      for (int q = 0; q < 4 * RT; ++q) coming[q] = at(c)[64 * q];
+  }
+};
+
+// Momentum, u into X, and the wavefront's share of u u^T.
+template <int RT>
+__device__ __forceinline__ void start_columns(const Columns<RT>& w, const MuonHyper& h, f32x16 (&g)[muon_upper(RT)]) {
+  const f16x8 unit[2] = {unit_slice(0, w.lane), unit_slice(1, w.lane)};
+#pragma unroll
+  for (int u = 0; u < muon_upper(RT); ++u) g[u] = zero16();
+  for (int c = w.first; c < w.end; c += muon_waves(RT)) {
+    f32x4 u[4 * RT];
+    const float s = scale_below(momentum_step<RT>(w.t, h, c * MUON_CHUNK, w.lane, w.room, u));
+    f32x4* x = w.at(c);
+#pragma unroll
+    for (int q = 0; q < 4 * RT; ++q) x[64 * q] = u[q];
+    Operand rows[RT][2];
+#pragma unroll
+    for (int a = 0; a < RT; ++a) {
+      const Operand in[2] = {split(u[4 * a] * s, u[4 * a + 1] * s), split(u[4 * a + 2] * s, u[4 * a + 3] * s)};
+      turn(in, unit, rows[a]);
+    }
+    const float back = inverse_power(s);  // (twice: its square may be below the smallest fp32)
+#pragma unroll
+    for (int b = 0; b < RT; ++b)
+#pragma unroll
+      for (int a = 0; a <= b; ++a) {
+        f32x16 part = zero16();
+#pragma unroll
+        for (int sl = 0; sl < 2; ++sl) add(part, rows[a][sl], rows[b][sl]);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) g[upper_at(a, b)][r] += part[r] * back * back;
+      }
+  }
+}
+
+// P = a I + b G + c G^2 as operands in LDS, its tile (t, a) at a RT + t (G's were there before).
+template <int RT>
+__device__ __forceinline__ Scales make_p(const float* gram, const MuonHyper& h, bool first, f32x4* lds, float* squares, int wave, int lane) {
+  constexpr int NW = muon_waves(RT);
+  // A wavefront has tiles (t, a) of G and of P, in results' layout: the operand for rows of tile a and slices of tile t.
+  constexpr int PT = (RT * RT + NW - 1) / NW;
+  f32x4 p[PT][4];
+#pragma unroll
+  for (int k = 0; k < PT; ++k)
+    if (wave + NW * k < RT * RT)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) p[k][q] = reinterpret_cast<const f32x4*>(gram)[(wave + NW * k) * 256 + q * 64 + lane];
+  float diagonal = 0.0f;
+#pragma unroll
+  for (int k = 0; k < (32 * RT + 63) / 64; ++k) {
+    const int d = lane + 64 * k, a = d >> 5, dd = d & 31;
+    if (d < 32 * RT) diagonal += gram[(a * RT + a) * 1024 + ((dd >> 3) * 64 + dd + 32 * ((dd >> 2) & 1)) * 4 + (dd & 3)];
+  }
+  Scales s(wave_sum(diagonal), h.eps, first);
+#pragma unroll
+  for (int k = 0; k < PT; ++k)
+    if (wave + NW * k < RT * RT) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        p[k][q] *= s.x_norm * s.x_norm;
+      put_operands(lds, wave + NW * k, lane, p[k], s.g);
+    }
+  __syncthreads();
+  float square = 0.0f;
+  const float g_back = inverse_power(s.g) * inverse_power(s.g);
+#pragma unroll
+  for (int k = 0; k < PT; ++k)
+    if (wave + NW * k < RT * RT) {
+      const int tt = (wave + NW * k) / RT, a = (wave + NW * k) % RT;
+      f32x16 g2 = zero16();
+#pragma unroll
+      for (int u = 0; u < RT; ++u)
+#pragma unroll
+        for (int sl = 0; sl < 2; ++sl) add(g2, operand_at(lds, u * RT + tt, sl, lane), operand_at(lds, u * RT + a, sl, lane));
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float one = (tt == a && 8 * q + 4 * (lane >> 5) + e == (lane & 31)) ? h.a : 0.0f;
+          p[k][q][e] = __builtin_fmaf(h.c, g2[4 * q + e] * g_back, __builtin_fmaf(h.b, p[k][q][e], one));
+          square = __builtin_fmaf(p[k][q][e], p[k][q][e], square);
+        }
+    }
+  square = wave_sum(square);
+  if (lane == 0) squares[wave] = square;
+  __syncthreads();  // (also: G has been read, and its place is free)
+  float p_bound = 0.0f;
+#pragma unroll
+  for (int k = 0; k < NW; ++k) p_bound += squares[k];
+  p_bound = __fsqrt_rn(p_bound) * 1.001f;
+  s.p = scale_below(p_bound);
+  s.y = scale_below(p_bound * s.x_bound);
+#pragma unroll
+  for (int k = 0; k < PT; ++k)
+    if (wave + NW * k < RT * RT) put_operands(lds, (wave + NW * k) % RT * RT + (wave + NW * k) / RT, lane, p[k], s.p);
+  __syncthreads();
+  return s;
+}
+
+// X <- P X on the wavefront's columns.  LAST: the result goes into the parameters, else back to X with its share of the next G.
+template <int RT, bool LAST>
+__device__ __forceinline__ void pass_columns(const Columns<RT>& w, const MuonHyper& h, const Scales& s, const f32x4* p, f32x4 (&coming)[4 * RT],
+                                             f32x16 (&g)[muon_upper(RT)]) {
+  constexpr int NW = muon_waves(RT);
+  const f16x8 unit[2] = {unit_slice(0, w.lane), unit_slice(1, w.lane)};
+#pragma unroll
+  for (int u = 0; u < muon_upper(RT); ++u) g[u] = zero16();
+  const float in_scale = s.x_norm * s.x, y_back = inverse_power(s.x) * inverse_power(s.p);
+  for (int c = w.first; c < w.end; c += NW) {
+    Operand x[RT][2];
+#pragma unroll
+    for (int a = 0; a < RT; ++a)
+#pragma unroll
+      for (int sl = 0; sl < 2; ++sl) x[a][sl] = split(coming[4 * a + 2 * sl] * in_scale, coming[4 * a + 2 * sl + 1] * in_scale);
+    w.request(c + NW, coming);
+    const Elements<RT> at(w.t, c * MUON_CHUNK, w.lane, w.room);
+    f32x4 param[4 * RT];
+    if constexpr (LAST) at.request(w.t.p, param);
+    Operand rows[RT][2];
+    // two row tiles at a time: their products alternate, and the operands of the next slice are read meanwhile
+    constexpr int PAIR = RT > 1 ? 2 : 1;
+    auto p_at = [&](int a, int k) { return operand_at(p, a * RT + (k >> 1), k & 1, w.lane); };  // rows of tile a, slice k
+#pragma unroll
+    for (int a0 = 0; a0 < RT; a0 += PAIR) {
+      f32x16 acc[PAIR];
+      Operand now[PAIR], next[PAIR];
+#pragma unroll
+      for (int j = 0; j < PAIR; ++j) {
+        acc[j] = zero16();
+        next[j] = p_at(a0 + j, 0);
+      }
+#pragma unroll
+      for (int k = 0; k < 2 * RT; ++k) {
+#pragma unroll
+        for (int j = 0; j < PAIR; ++j) {
+          now[j] = next[j];
+          if (k + 1 < 2 * RT) next[j] = p_at(a0 + j, k + 1);
+        }
+        const Operand& xk = x[k >> 1][k & 1];
+#pragma unroll
+        for (int j = 0; j < PAIR; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[j].hi, xk.hi, acc[j], 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < PAIR; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[j].hi, xk.lo, acc[j], 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < PAIR; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[j].lo, xk.hi, acc[j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (LAST && a0 == 0) at.settle(param);
+#pragma unroll
+      for (int j = 0; j < PAIR; ++j) {
+        const int a = a0 + j;
+        f32x4 y[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) y[q] = quad_of(acc[j], q) * y_back;
+        if constexpr (LAST) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) param[4 * a + q][e] = __builtin_fmaf(param[4 * a + q][e], h.decay, -w.t.step_size * y[q][e]);
+        } else {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) w.at(c)[64 * (4 * a + q)] = y[q];
+          const Operand in[2] = {split(y[0] * s.y, y[1] * s.y), split(y[2] * s.y, y[3] * s.y)};
+          turn(in, unit, rows[a]);
+        }
+      }
+    }
+    if constexpr (LAST) {
+      __builtin_amdgcn_sched_barrier(0);
+      at.store(w.t.p, param);
+    } else {
+      add_gram<RT>(g, rows);
+    }
+  }
+  if constexpr (!LAST) {
+    const float back = inverse_power(s.y) * inverse_power(s.y);
+#pragma unroll
+    for (int u = 0; u < muon_upper(RT); ++u)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) g[u][r] *= back;
+  }
+}
 
 }  // namespace
 
-// Momentum, u into X, and the blocks' shares of u u^T.
 template <int RT>
-__global__ __launch_bounds__(64 * muon_waves(RT)) void muon_start_kernel(const MuonTable table, const MuonHyper h, float* ws) {
-  constexpr int NW = muon_waves(RT), NT = 64 * NW, LO = muon_x_halves(RT), Q = Gram<RT>::Q;
-  __shared__ __align__(16) _Float16 xs[2 * LO];
-  __shared__ float wave_max[NW];
-  const Where w = muon_where(table);
-  const MuonTensor& t = *w.t;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const bool wide = t.rows <= t.cols;
-  const Gram<RT> gram(t.tiles, wave, lane, XLD);
-  f32x4 sum[Q][4];
-#pragma unroll
-  for (int q = 0; q < Q; ++q)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) sum[q][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int c = w.c0; c < w.c1; ++c) {
-    float* x = ws + t.x + (size_t)c * t.tiles * 32 * MUON_CHUNK;
-    const bool part = c == w.c0 || c + 1 == t.chunks;  // rows or columns outside the matrix are not zero yet
-    if (part) {
-      for (int e = threadIdx.x; e < 2 * LO / 8; e += NT) reinterpret_cast<f32x4*>(xs)[e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-    // (memory outside the matrix: the few elements that the pieces below do not write)
-    const int rows_in = wide ? t.rows : t.cols, cols_in = min(MUON_CHUNK, (wide ? t.cols : t.rows) - c * MUON_CHUNK);
-    if (rows_in < 32 * t.tiles || cols_in < MUON_CHUNK)
-      for (int e = threadIdx.x; e < 32 * t.tiles * MUON_CHUNK; e += NT) {
-        const int i = e / MUON_CHUNK, n = e % MUON_CHUNK;
-        if (i >= rows_in || n >= cols_in) x[kept_at(i, n)] = 0.0f;
-      }
-    auto momentum = [&](auto width) {
-      constexpr int W = decltype(width)::value, K = 32 * RT * MUON_CHUNK / (NT * W);
-      Piece<W> g[K], m[K];
-      float most = 0.0f;
-      each_piece<RT, NT, W>(t, c, [&](int k, size_t at, int, int) {
-        g[k] = load_piece<W>(t.g + at);
-        m[k] = load_piece<W>(t.m + at);
-      });
-      each_piece<RT, NT, W>(t, c, [&](int k, size_t at, int, int) {
-#pragma unroll
-        for (int e = 0; e < W; ++e) m[k].v[e] = __builtin_fmaf(h.momentum, m[k].v[e], g[k].v[e]);
-        store_piece<W>(t.m + at, m[k]);
-        if (h.zero_grads) store_piece<W>(t.g + at, Piece<W>{});
-#pragma unroll
-        for (int e = 0; e < W; ++e) {
-          if (h.nesterov) m[k].v[e] = __builtin_fmaf(h.momentum, m[k].v[e], g[k].v[e]);
-          most = fmaxf(most, fabsf(m[k].v[e]));
-        }
-      });
-#pragma unroll
-      for (int off = 32; off >= 1; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, 64));
-      if (lane == 0) wave_max[wave] = most;
-      __syncthreads();  // (the planes are cleared, and those of the chunk before have been read)
-#pragma unroll
-      for (int k = 0; k < NW; ++k) most = fmaxf(most, wave_max[k]);
-      const float s = scale_below(most);
-      each_piece<RT, NT, W>(t, c, [&](int k, size_t, int i, int n) {
-        if (W == 4 && wide) {
-          f32x4 v;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = m[k].v[e % W];
-          *reinterpret_cast<f32x4*>(x + kept_at(i, n)) = v;
-          put4(xs + i * XLD + n, LO, v * s);
-        } else {
-#pragma unroll
-          for (int e = 0; e < W; ++e) {
-            x[kept_at(i + e, n)] = m[k].v[e];
-            put1(xs + (i + e) * XLD + n, LO, m[k].v[e] * s);
-          }
-        }
-      });
-      return s;
-    };
-    const float s = t.cols % 4 == 0 ? momentum(std::integral_constant<int, 4>{}) : momentum(std::integral_constant<int, 1>{});
-    __syncthreads();
-    const float back = inverse_power(s);  // (twice: its square may be below the smallest fp32)
-#pragma unroll
-    for (int q = 0; q < Q; ++q)
-      if (gram.live(q)) {
-        Tile p;
-        p.clear();
-        add_rows(p, xs + gram.at_a[q], xs + gram.at_b[q], LO, MUON_CHUNK / 16);
-#pragma unroll
-        for (int g = 0; g < 4; ++g) sum[q][g] += p.quad(g, back) * back;
-      }
-    __syncthreads();  // the next chunk's wave_max and planes
-  }
-  f32x4* out = reinterpret_cast<f32x4*>(ws + t.partial) + (size_t)w.slice * t.tiles * t.tiles * 256;
-#pragma unroll
-  for (int q = 0; q < Q; ++q)
-    if (gram.live(q))
-#pragma unroll
-      for (int g = 0; g < 4; ++g) out[((wave + NW * q) * 4 + g) * 64 + lane] = sum[q][g];
+__global__ __launch_bounds__(64 * muon_waves(RT), 1) void muon_start_kernel(const MuonTable table, const MuonHyper h, float* ws) {
+  extern __shared__ __align__(16) f32x4 lds[];
+  const int ti = muon_find(table.block0), slice = (int)blockIdx.x - table.block0[ti];
+  const MuonTensor& t = table.t[ti];
+  const Columns<RT> w(t, ws, slice * table.per_block, min(t.chunks, (slice + 1) * table.per_block), reinterpret_cast<float*>(lds));
+  f32x16 g[muon_upper(RT)];
+  start_columns<RT>(w, h, g);
+  store_share<RT>(g, lds, reinterpret_cast<f32x4*>(ws + t.partial) + (size_t)slice * muon_upper(RT) * 256, w.wave, w.lane);
 }
 
-// G = sum of the blocks' shares: 32 pieces of 16 bytes a block, their shares dealt to eight groups of threads.
+// G = sum of the blocks' shares, upper tiles, and their mirror images: 32 pieces of 16 bytes a block, their shares dealt to
+// eight groups of threads.
+template <int RT>
 __global__ __launch_bounds__(256) void muon_reduce_kernel(const MuonTable table, float* ws) {
   __shared__ f32x4 part[8][32];
   const int ti = muon_find(table.reduce0);
   const MuonTensor& t = table.t[ti];
   const int slices = (t.chunks + table.per_block - 1) / table.per_block;
   const int e = threadIdx.x & 31, group = threadIdx.x >> 5;
-  const size_t pieces = (size_t)t.tiles * t.tiles * 256, at = (size_t)(blockIdx.x - table.reduce0[ti]) * 32 + e;
+  constexpr int pieces = muon_upper(RT) * 256;
+  const int at = (int)(blockIdx.x - table.reduce0[ti]) * 32 + e;
   const f32x4* src = reinterpret_cast<const f32x4*>(ws + t.partial) + at;
   const int per = (slices + 7) / 8, z0 = min(slices, group * per), z1 = min(slices, z0 + per);
   f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -317,216 +610,109 @@ __global__ __launch_bounds__(256) void muon_reduce_kernel(const MuonTable table,
   for (int z = z0; z < z1; ++z) v += src[(size_t)z * pieces];
   part[group][e] = v;
   __syncthreads();
-  if (group == 0) {
+  if (group > 0) return;
 #pragma unroll
-    for (int k = 1; k < 8; ++k) v += part[k][e];
-    reinterpret_cast<f32x4*>(ws + t.gram)[at] = v;
-  }
+  for (int k = 1; k < 8; ++k) v += part[k][e];
+  const int u = at >> 8, q = (at >> 6) & 3, lane = at & 63;
+  int b = 0;
+  while ((b + 1) * (b + 2) / 2 <= u) ++b;
+  const int a = u - b * (b + 1) / 2;
+  put_gram<RT>(ws + t.gram, a, b, q, lane, v);
 }
 
-// One step of the iteration on the block's chunks.  FIRST: X holds u, whose norm comes off here.  LAST: the result goes into the
-// parameters, else back to X with the shares of the next G.
-template <int RT, bool FIRST, bool LAST>
-__global__ __launch_bounds__(64 * muon_waves(RT)) void muon_pass_kernel(const MuonTable table, const MuonHyper h, float* ws) {
-  constexpr int NW = muon_waves(RT), NT = 64 * NW, PLD = muon_pld(RT), Q = Gram<RT>::Q;
-  constexpr int XLO = muon_x_halves(RT), PLO = muon_p_halves(RT);
-  extern __shared__ __align__(16) _Float16 lds[];
-  _Float16* xs = lds;           // [hi, lo][32 RT][XLD]: X
-  _Float16* ys = xs + 2 * XLO;  // P X
-  _Float16* ps = ys + 2 * XLO;  // [hi, lo][32 RT][PLD]: G, then P
-  const Where w = muon_where(table);
-  const MuonTensor& t = *w.t;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lo5 = lane & 31, hi1 = lane >> 5;
-  const int it = wave >> 1, nt = wave & 1;  // the wavefront's tile of a chunk
-  const bool mine = it < t.tiles;
+// One step of the iteration.  first: X holds u, whose norm comes off here.
+template <int RT, bool LAST>
+__global__ __launch_bounds__(64 * muon_waves(RT), 1) void muon_pass_kernel(const MuonTable table, const MuonHyper h, bool first, float* ws) {
+  extern __shared__ __align__(16) f32x4 lds[];
+  __shared__ float squares[muon_waves(RT)];
+  const int ti = muon_find(table.block0), slice = (int)blockIdx.x - table.block0[ti];
+  const MuonTensor& t = table.t[ti];
+  const Columns<RT> w(t, ws, slice * table.per_block, min(t.chunks, (slice + 1) * table.per_block),
+                      reinterpret_cast<float*>(lds) + muon_p_lds(RT) / 4);
+  // The columns that come next are on their way: the first ones while P is made, later ones while those before are worked on.
+  f32x4 coming[4 * RT];
+#pragma unroll
+  for (int q = 0; q < 4 * RT; ++q) coming[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  w.request(w.first, coming);
+  const Scales s = make_p<RT>(ws + t.gram, h, first, lds, squares, w.wave, w.lane);
+  f32x16 g[muon_upper(RT)];
+  pass_columns<RT, LAST>(w, h, s, lds, coming, g);
+  if constexpr (!LAST)
+    store_share<RT>(g, lds, reinterpret_cast<f32x4*>(ws + t.partial) + (size_t)slice * muon_upper(RT) * 256, w.wave, w.lane);
+}
 
-  // ---- requests: G's diagonal and tiles, the first chunk --------------------------------------
-  const float* gram_at = ws + t.gram;
-  float diagonal = 0.0f;
+// All steps of a matrix in one block, G in its LDS: the launches above take 5 to 7 us each however little there is to do.
+template <int RT>
+__global__ __launch_bounds__(64 * muon_waves(RT), 1) void muon_alone_kernel(const MuonTable table, const MuonHyper h, int steps, float* ws) {
+  extern __shared__ __align__(16) f32x4 lds[];  // operands of G and P, then G, then the shares or the rooms for tall matrices
+  __shared__ float squares[muon_waves(RT)];
+  const MuonTensor& t = table.t[blockIdx.x];
+  f32x4* shares = lds + 2 * muon_p_lds(RT) / 16;
+  float* gram = reinterpret_cast<float*>(lds) + muon_p_lds(RT) / 4;
+  const Columns<RT> w(t, ws, 0, t.chunks, reinterpret_cast<float*>(shares));
+  f32x16 g[muon_upper(RT)];
+  start_columns<RT>(w, h, g);
+  f32x4 coming[4 * RT];
+  auto next_p = [&](bool first) {
+    int lane = w.lane;
+    asm volatile("" : "+v"(lane));  // (else the places in LDS that depend on it are held in registers throughout)
+    add_shares<RT>(g, shares, w.wave, lane);
+    if (w.wave == 0)
 #pragma unroll
-  for (int k = 0; k < (32 * RT + 63) / 64; ++k) {
-    const int d = lane + 64 * k, a = d >> 5, dd = d & 31;
-    if (d < 32 * t.tiles)
-      diagonal += gram_at[(((a * t.tiles + a) * 4 + (dd >> 3)) * 64 + dd + 32 * ((dd >> 2) & 1)) * 4 + (dd & 3)];
-  }
-  const Gram<RT> square(t.tiles, wave, lane, PLD);
-  f32x4 g[Q][4];
+      for (int b = 0; b < RT; ++b)
 #pragma unroll
-  for (int q = 0; q < Q; ++q)
-    if (square.live(q))
+        for (int a = 0; a <= b; ++a)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) g[q][k] = reinterpret_cast<const f32x4*>(gram_at)[((wave + NW * q) * 4 + k) * 64 + lane];
-  // The chunk that comes next, on its way: the first one while P is made, each later one while the one before is worked on.
-  f32x4 coming[4];
-  auto chunk_at = [&](int c) {
-    return reinterpret_cast<f32x4*>(ws + t.x) + ((size_t)c * t.tiles * 2 + wave) * 256 + lane;
+          for (int q = 0; q < 4; ++q) put_gram<RT>(gram, a, b, q, lane, quad_of(g[upper_at(a, b)], q));
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 4 * RT; ++q) coming[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    w.request(w.first, coming);
+    return make_p<RT>(gram, h, first, lds, squares, w.wave, lane);
   };
-  auto request = [&](int c) {
-    if (mine)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) coming[k] = chunk_at(c)[64 * k];
-  };
-  request(w.c0);
-
-  // ---- scales ---------------------------------------------------------------------------------
-  float trace = diagonal;
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) trace += __shfl_xor(trace, off, 64);
-  float x_norm = 1.0f;  // times X as it is kept
-  if constexpr (FIRST) {
-    x_norm = 1.0f / (__fsqrt_rn(trace) + h.eps);
-#pragma unroll
-    for (int q = 0; q < Q; ++q)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) g[q][k] *= x_norm * x_norm;
+  for (int k = 0; k + 1 < steps; ++k) {
+    const Scales s = next_p(k == 0);
+    pass_columns<RT, false>(w, h, s, lds, coming, g);
   }
-  const float x_bound = (__fsqrt_rn(trace) + kLostNorm) * x_norm;
-  trace *= x_norm * x_norm;
-  const float p_bound = fabsf(h.a) + fabsf(h.b) * trace + fabsf(h.c) * trace * trace;
-  const float s_g = scale_below(trace), s_p = scale_below(p_bound), s_x = scale_below(x_bound),
-              s_y = scale_below(1.001f * p_bound * x_bound);
-
-  // ---- P = a I + b G + c G^2 ------------------------------------------------------------------
-  // A lane's quads of tile (a, b) go to rows 32 b + lane % 32: the transposed place, where a symmetric matrix has the same
-  auto put_tile = [&](int q, int k, const f32x4& v) {
-    const int id = wave + NW * q, a = id / t.tiles, b = id - a * t.tiles;
-    put4(ps + (32 * b + lo5) * PLD + 32 * a + 8 * k + 4 * hi1, PLO, v);
-  };
-#pragma unroll
-  for (int q = 0; q < Q; ++q)
-    if (square.live(q))
-#pragma unroll
-      for (int k = 0; k < 4; ++k) put_tile(q, k, g[q][k] * s_g);
-  __syncthreads();
-  const float g_back = inverse_power(s_g) * inverse_power(s_g);
-#pragma unroll
-  for (int q = 0; q < Q; ++q)
-    if (square.live(q)) {
-      const int id = wave + NW * q, a = id / t.tiles, b = id - a * t.tiles;
-      Tile p;
-      p.clear();
-      add_rows(p, ps + square.at_a[q], ps + square.at_b[q], PLO, 2 * t.tiles);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const f32x4 g2 = p.quad(k, g_back);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float one = (a == b && 8 * k + 4 * hi1 + e == lo5) ? h.a : 0.0f;
-          g[q][k][e] = __builtin_fmaf(h.c, g2[e], __builtin_fmaf(h.b, g[q][k][e], one));
-        }
-      }
-    }
-  __syncthreads();
-#pragma unroll
-  for (int q = 0; q < Q; ++q)
-    if (square.live(q))
-#pragma unroll
-      for (int k = 0; k < 4; ++k) put_tile(q, k, g[q][k] * s_p);
-
-  // ---- the block's columns: X <- P X ----------------------------------------------------------
-  const Gram<RT> gram(t.tiles, wave, lane, XLD);
-  Tile next_g[Q];
-#pragma unroll
-  for (int q = 0; q < Q; ++q) next_g[q].clear();
-  const int place = (32 * it + lo5) * XLD + 32 * nt + 4 * hi1;  // + 8 k: the lane's quads in a plane
-  const float in_scale = x_norm * s_x, y_back = inverse_power(s_x) * inverse_power(s_p);
-  for (int c = w.c0; c < w.c1; ++c) {
-    if (mine)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) put4(xs + place + 8 * k, XLO, coming[k] * in_scale);
-    __syncthreads();  // (also: everybody is done with the columns before)
-    if (c + 1 < w.c1) request(c + 1);
-    f32x4 y[4];
-    if (mine) {
-      Tile p;
-      p.clear();
-      const _Float16* rows = ps + (32 * it + lo5) * PLD + 8 * hi1;
-#pragma unroll 2
-      for (int s = 0; s < 2 * t.tiles; ++s) {
-        const _Float16* cols = xs + 16 * s * XLD + 32 * nt;
-        p.add(read_columns(cols, lane), read_columns(cols + XLO, lane), read8(rows + 16 * s), read8(rows + 16 * s + PLO));
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) y[k] = p.quad(k, y_back);
-    }
-    if constexpr (LAST) {
-      // through LDS as fp32 (in the room of P X), so that the parameters are read and written in whole rows
-      float* out = reinterpret_cast<float*>(ys);
-      constexpr int OLD = MUON_CHUNK + 4;
-      static_assert(32 * RT * OLD * 4 <= 2 * XLO * 2, "the tile fits");
-      if (mine)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          *reinterpret_cast<f32x4*>(out + (32 * it + lo5) * OLD + 32 * nt + 8 * k + 4 * hi1) = y[k];
-      auto update = [&](auto width) {
-        constexpr int W = decltype(width)::value, K = 32 * RT * MUON_CHUNK / (NT * W);
-        Piece<W> p[K];
-        each_piece<RT, NT, W>(t, c, [&](int k, size_t at, int, int) { p[k] = load_piece<W>(t.p + at); });
-        __syncthreads();
-        each_piece<RT, NT, W>(t, c, [&](int k, size_t at, int i, int n) {
-          const int step = t.rows <= t.cols ? 1 : OLD;
-#pragma unroll
-          for (int e = 0; e < W; ++e) p[k].v[e] = __builtin_fmaf(p[k].v[e], h.decay, -t.step_size * out[i * OLD + n + e * step]);
-          store_piece<W>(t.p + at, p[k]);
-        });
-      };
-      if (t.cols % 4 == 0) update(std::integral_constant<int, 4>{});
-      else update(std::integral_constant<int, 1>{});
-    } else {
-      if (mine)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          chunk_at(c)[64 * k] = y[k];
-          put4(ys + place + 8 * k, XLO, y[k] * s_y);
-        }
-      __syncthreads();
-#pragma unroll
-      for (int q = 0; q < Q; ++q)
-        if (gram.live(q)) add_rows(next_g[q], ys + gram.at_a[q], ys + gram.at_b[q], XLO, MUON_CHUNK / 16);
-    }
-  }
-  if constexpr (!LAST) {
-    const float back = inverse_power(s_y) * inverse_power(s_y);
-    f32x4* out = reinterpret_cast<f32x4*>(ws + t.partial) + (size_t)w.slice * t.tiles * t.tiles * 256;
-#pragma unroll
-    for (int q = 0; q < Q; ++q)
-      if (gram.live(q))
-#pragma unroll
-        for (int k = 0; k < 4; ++k) out[((wave + NW * q) * 4 + k) * 64 + lane] = next_g[q].quad(k, back);
-  }
+  const Scales s = next_p(steps == 1);
+  pass_columns<RT, true>(w, h, s, lds, coming, g);
 }
 
 namespace {
 
-template <int RT, bool FIRST, bool LAST>
-hipError_t launch_pass(const MuonTable& t, const MuonHyper& h, float* ws, hipStream_t st) {
-  static std::atomic<uint64_t> granted{0};  // per instantiation
-  auto kern = muon_pass_kernel<RT, FIRST, LAST>;
-  constexpr size_t lds = muon_pass_lds(RT);
+template <typename Kernel, typename... Args>
+hipError_t launch(Kernel kern, int blocks, int rt, size_t lds, std::atomic<uint64_t>& granted, hipStream_t st, const Args&... args) {
   if (hipError_t e = grant_dynamic_lds(reinterpret_cast<const void*>(kern), (int)lds, granted); e != hipSuccess) return e;
-  kern<<<t.blocks, 64 * muon_waves(RT), lds, st>>>(t, h, ws);
+  kern<<<blocks, 64 * muon_waves(rt), lds, st>>>(args...);
   return hipGetLastError();
 }
 
 template <int RT>
 hipError_t launch_steps(const MuonTable& t, const MuonHyper& h, int steps, float* ws, hipStream_t st) {
-  muon_start_kernel<RT><<<t.blocks, 64 * muon_waves(RT), 0, st>>>(t, h, ws);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  static std::atomic<uint64_t> granted[3];
+  if (hipError_t e = launch(muon_start_kernel<RT>, t.blocks, RT, muon_start_lds(RT), granted[0], st, t, h, ws); e != hipSuccess) return e;
   for (int k = 0; k < steps; ++k) {
-    muon_reduce_kernel<<<t.reduce_blocks, 256, 0, st>>>(t, ws);
+    muon_reduce_kernel<RT><<<t.reduce_blocks, 256, 0, st>>>(t, ws);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    const bool first = k == 0, last = k + 1 == steps;
-    const hipError_t e = first ? (last ? launch_pass<RT, true, true>(t, h, ws, st) : launch_pass<RT, true, false>(t, h, ws, st))
-                               : (last ? launch_pass<RT, false, true>(t, h, ws, st) : launch_pass<RT, false, false>(t, h, ws, st));
+    const hipError_t e = k + 1 < steps ? launch(muon_pass_kernel<RT, false>, t.blocks, RT, muon_pass_lds(RT, false), granted[1], st, t, h, k == 0, ws)
+                                       : launch(muon_pass_kernel<RT, true>, t.blocks, RT, muon_pass_lds(RT, true), granted[2], st, t, h, k == 0, ws);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
+template <int RT>
+hipError_t launch_alone(const MuonTable& t, const MuonHyper& h, int steps, float* ws, hipStream_t st) {
+  static std::atomic<uint64_t> granted{0};
+  return launch(muon_alone_kernel<RT>, t.n, RT, muon_alone_lds(RT), granted, st, t, h, steps, ws);
+}
+
 }  // namespace
 
 hipError_t launch_muon(const MuonTable& t, const MuonHyper& h, int steps, float* ws, hipStream_t st) {
-  return t.max_tiles > 2 ? launch_steps<4>(t, h, steps, ws, st) : launch_steps<2>(t, h, steps, ws, st);
+  if (t.alone) return t.tiles == 2 ? launch_alone<2>(t, h, steps, ws, st) : launch_alone<1>(t, h, steps, ws, st);
+  if (t.tiles > 2) return launch_steps<4>(t, h, steps, ws, st);
+  return t.tiles == 2 ? launch_steps<2>(t, h, steps, ws, st) : launch_steps<1>(t, h, steps, ws, st);
 }
 
 }  // namespace qalora

@@ -7,30 +7,37 @@ namespace qalora {
 
 constexpr int MUON_MAX_TENSORS = 32;
 constexpr int MUON_MAX_SHORT = 128;  // shorter side of a matrix: its Gram matrix lives in one compute unit's LDS
-constexpr int MUON_CHUNK = 64;       // entries of the longer side that a block works on at a time
+constexpr int MUON_MAX_LONG = 1 << 27;  // a lane's distance in bytes from its wavefront's first element fits 32 bits
+constexpr int MUON_CHUNK = 32;       // entries of the longer side that a wavefront works on at a time
 
 // One matrix, seen as X [shorter side x longer side].
 struct MuonTensor {
   float *p, *g, *m;      // [rows, cols]
   int rows, cols;
-  int tiles;             // 32-row tiles of the shorter side
   int chunks;            // of the longer side
   float step_size;       // lr times the shape's scale
-  size_t x;              // floats from the workspace's start: X as [chunks][32 tiles][MUON_CHUNK]
+  size_t x;              // floats from the workspace's start: X as [chunks][tiles] of 32 x MUON_CHUNK
   size_t gram;           // the Gram matrix: [tiles][tiles] of 32 x 32
-  size_t partial;        // each block's share of it
+  size_t partial;        // each block's share of it: the upper tiles
 };
 struct MuonTable {
-  int n, blocks, reduce_blocks, per_block, max_tiles;
+  int n, blocks, reduce_blocks, per_block;
+  int tiles;                      // 32-row tiles that every X has: 1, 2 or 4, rows beyond a shorter side being zero
+  bool alone;                     // a block does all steps of a matrix
   int block0[MUON_MAX_TENSORS];   // first block of the launches over X; blocks of `per_block` chunks
   int reduce0[MUON_MAX_TENSORS];  // first block of the launch that adds the blocks' Gram matrices
   MuonTensor t[MUON_MAX_TENSORS];
 };
 constexpr int MUON_REDUCE_BLOCKS_PER_TILE = 8;  // (muon_reduce_kernel: 32 of a tile's 256 16-byte pieces a block)
+constexpr int muon_upper_tiles(int tiles) { return tiles * (tiles + 1) / 2; }
 
-// Blocks over X: about as many as the chip holds at once (a block first squares the Gram matrix, so more of them only
-// repeat that; 143 KB of LDS with more than 64 rows, 55 KB below).
-constexpr int muon_target_blocks(int max_tiles) { return max_tiles > 2 ? 256 : 512; }
+// A block's wavefronts take `muon_waves` chunks at a time; blocks over X as many as there are compute units at most (a block first
+// makes P from the Gram matrix, and leaves a share of the next: more of them only repeat that).
+constexpr int muon_waves_of(int tiles) { return tiles > 2 ? 4 : 8; }
+constexpr int MUON_BLOCKS = 256;
+// One launch, a block for each matrix, where the longest has this many 32 x 32 tiles of X at most.  Two matrices, 5 steps, us (one
+// launch against eleven): 32 x 512 27 / 52, 1024 42 / 53, 2048 69 / 54; 64 x 512 53 / 70, 1024 84 / 71.
+constexpr int MUON_ALONE_TILES = 32;
 
 // Fills in the table from rows[] and cols[]; returns the workspace's floats, 0 where the list is not acceptable
 // (`unsupported` says whether a matrix has both sides above MUON_MAX_SHORT, rather than a bad argument).
@@ -39,38 +46,40 @@ inline size_t muon_table(int n, const int32_t* rows, const int32_t* cols, MuonTa
   if (n < 1 || n > MUON_MAX_TENSORS || !rows || !cols) return 0;
   long long chunks = 0;
   table.n = n;
-  table.max_tiles = 0;
+  int longest = 0, most_chunks = 0;
   for (int i = 0; i < n; ++i) {
     if (rows[i] < 1 || cols[i] < 1) return 0;
+    if (rows[i] > MUON_MAX_LONG || cols[i] > MUON_MAX_LONG) unsupported = true;
     MuonTensor& t = table.t[i];
     t.rows = rows[i];
     t.cols = cols[i];
     const int shorter = rows[i] < cols[i] ? rows[i] : cols[i], longer = rows[i] < cols[i] ? cols[i] : rows[i];
     if (shorter > MUON_MAX_SHORT) unsupported = true;
-    t.tiles = (shorter + 31) / 32;
+    if (shorter > longest) longest = shorter;
     t.chunks = longer / MUON_CHUNK + (longer % MUON_CHUNK ? 1 : 0);
-    if (t.tiles > table.max_tiles) table.max_tiles = t.tiles;
     chunks += t.chunks;
+    if (t.chunks > most_chunks) most_chunks = t.chunks;
   }
   if (unsupported) return 0;
-  const int target = muon_target_blocks(table.max_tiles);
-  table.per_block = (int)((chunks + target - 1) / target);
+  table.tiles = longest > 64 ? 4 : (longest > 32 ? 2 : 1);
+  table.alone = table.tiles <= 2 && most_chunks <= MUON_ALONE_TILES / table.tiles;
+  const int waves = muon_waves_of(table.tiles), upper = muon_upper_tiles(table.tiles);
+  table.per_block = (int)((chunks + MUON_BLOCKS * waves - 1) / (MUON_BLOCKS * waves)) * waves;
   size_t floats = 0;
   table.blocks = table.reduce_blocks = 0;
   for (int i = 0; i < n; ++i) {
     MuonTensor& t = table.t[i];
     const int blocks = (t.chunks + table.per_block - 1) / table.per_block;
-    const size_t gram = (size_t)t.tiles * t.tiles * 1024;
     table.block0[i] = table.blocks;
     table.reduce0[i] = table.reduce_blocks;
     table.blocks += blocks;
-    table.reduce_blocks += t.tiles * t.tiles * MUON_REDUCE_BLOCKS_PER_TILE;
+    table.reduce_blocks += upper * MUON_REDUCE_BLOCKS_PER_TILE;
     t.x = floats;
-    floats += (size_t)t.chunks * t.tiles * 32 * MUON_CHUNK;
+    floats += (size_t)t.chunks * table.tiles * 32 * MUON_CHUNK;
     t.gram = floats;
-    floats += gram;
+    floats += (size_t)table.tiles * table.tiles * 1024;
     t.partial = floats;
-    floats += (size_t)blocks * gram;
+    floats += (size_t)blocks * upper * 1024;
   }
   for (int i = n; i < MUON_MAX_TENSORS; ++i) table.block0[i] = table.reduce0[i] = INT32_MAX;
   return floats;

@@ -18,11 +18,11 @@ extern "C" long long plan(int n, const int* rows, const int* cols, int* unsuppor
   return (long long)floats;
 }
 extern "C" void totals(long long* out) {
-  out[0] = table.blocks; out[1] = table.reduce_blocks; out[2] = table.per_block; out[3] = table.max_tiles;
+  out[0] = table.blocks; out[1] = table.reduce_blocks; out[2] = table.per_block; out[3] = table.tiles; out[4] = table.alone;
 }
 extern "C" void tensor(int i, long long* out) {
   const MuonTensor& t = table.t[i];
-  out[0] = t.tiles; out[1] = t.chunks; out[2] = table.block0[i]; out[3] = table.reduce0[i];
+  out[0] = table.tiles; out[1] = t.chunks; out[2] = table.block0[i]; out[3] = table.reduce0[i];
   out[4] = (long long)t.x; out[5] = (long long)t.gram; out[6] = (long long)t.partial;
 }
 """
@@ -38,7 +38,7 @@ def plan(tmp_path_factory):
         arr = ctypes.c_int * max(n, 1)
         u = ctypes.c_int()
         floats = lib.plan(n, arr(*(r for r, _ in shapes)), arr(*(c for _, c in shapes)), ctypes.byref(u))
-        tot, ts = (ctypes.c_longlong * 4)(), []
+        tot, ts = (ctypes.c_longlong * 5)(), []
         lib.totals(tot)
         for i in range(n if floats else 0):
             t = (ctypes.c_longlong * 7)()
@@ -52,26 +52,30 @@ def plan(tmp_path_factory):
 def test_table_covers_every_matrix_once(plan):
     rng = random.Random(3)
     lists = [[(rng.randint(1, 128), rng.randint(1, 30000)) for _ in range(rng.randint(1, 32))] for _ in range(200)]
-    lists += [[(1, 1)], [(128, 2 ** 31 - 1)], [(2 ** 31 - 1, 1)], [(128, 128)] * 32, [(64, 1000000)] * 32]
+    lists += [[(rng.randint(1, 64), rng.randint(1, 1200)) for _ in range(rng.randint(1, 4))] for _ in range(100)]
+    lists += [[(1, 1)], [(128, 2 ** 27)], [(2 ** 27, 1)], [(128, 128)] * 32, [(64, 1000000)] * 32]
     for shapes in lists:
         shapes = [s if rng.random() < 0.5 else s[::-1] for s in shapes]
-        floats, unsupported, (blocks, reduce_blocks, per_block, max_tiles), ts = plan(shapes)
+        floats, unsupported, (blocks, reduce_blocks, per_block, tiles, alone), ts = plan(shapes)
         assert floats > 0 and not unsupported
         end = block = reduce = 0
-        for (rows, cols), (tiles, chunks, block0, reduce0, x, gram, partial) in zip(shapes, ts):
+        for (rows, cols), (_, chunks, block0, reduce0, x, gram, partial) in zip(shapes, ts):
             short, long = min(rows, cols), max(rows, cols)
-            assert 32 * (tiles - 1) < short <= 32 * tiles <= 32 * max_tiles and 64 * (chunks - 1) < long <= 64 * chunks
-            slices, g = -(-chunks // per_block), tiles * tiles * 1024
+            assert tiles in (1, 2, 4) and short <= 32 * tiles and 32 * (chunks - 1) < long <= 32 * chunks
+            slices, upper = -(-chunks // per_block), tiles * (tiles + 1) // 2
             assert (block0, reduce0, x) == (block, reduce, end)           # regions follow each other without a gap
-            assert gram == x + chunks * tiles * 32 * 64 and partial == gram + g
-            end, block, reduce = partial + slices * g, block + slices, reduce + 8 * tiles * tiles
+            assert gram == x + chunks * tiles * 32 * 32 and partial == gram + tiles * tiles * 1024
+            end, block, reduce = partial + slices * upper * 1024, block + slices, reduce + 8 * upper
             assert x % 4 == gram % 4 == partial % 4 == 0                  # 16-byte accesses
+        assert alone == (tiles < 4 and max(max(s) for s in shapes) <= 1024 // tiles)
+        assert max(min(s) for s in shapes) > (32 * tiles // 2 if tiles > 1 else 0)
         assert (floats, blocks, reduce_blocks) == (end, block, reduce) and blocks < 2 ** 31
 
 
 def test_unacceptable_lists(plan):
     assert plan([(129, 129)])[:2] == (0, True)
     assert plan([(8, 8), (300, 129)])[:2] == (0, True)
+    assert plan([(8, 2 ** 27 + 1)])[:2] == (0, True) and plan([(2 ** 31 - 1, 8)])[:2] == (0, True)
     for shapes in ([], [(0, 4)], [(4, 0)], [(-1, 4)], [(4, 4)] * 33):
         assert plan(shapes)[:2] == (0, False)
 
