@@ -418,13 +418,14 @@ int qalora_adamw_step(const qalora_adamw* hp, int step, int n_tensors, float* co
  * (3.4445, -4.7750, 2.0315) with five steps are the published coefficients (K. Jordan, Muon, 2024): they bring singular
  * values from 2e-3 of |u|_F on to 0.7 .. 1.2; (1.5, -0.5, 0) converges to one, but slowly.
  * scale: 1; sqrt(max(1, rows / cols)); or 0.2 sqrt(max(rows, cols)), the mean square of an AdamW step.
- * params, grads, momentum: HOST arrays of n_tensors DEVICE pointers (fp32, row-major, 16-byte aligned, no two the same);
+ * params, grads, momentum: HOST arrays of n_tensors DEVICE pointers (fp32, row-major, 16-byte aligned, no two overlapping:
+ * QALORA_EINVAL);
  * params and momentum are updated in place; grads are read, and set to zero afterwards if zero_grads != 0.
  * rows, cols: HOST arrays.  The shorter side is at most QALORA_MUON_MAX_SHORT (the rank of an adapter;
  * QALORA_EUNSUPPORTED otherwise), the longer one at most 2^27.  eps > 0; a matrix of zeros gets the update zero.
  * A matrix with an infinity or a NaN in u becomes NaN, the others do not see it.
  * ws: qalora_muon_workspace_bytes(n_tensors, rows, cols) bytes (0 for a list that is not acceptable): what the matrices take
- * themselves with every shorter side padded to 32, 64 or 128 (the same for all), and up to 21 MB.  fp32 arithmetic, sums in a fixed order: a step is bit-reproducible.  Errors of the sums, about 2^-24 of
+ * themselves with every shorter side padded to 32, 64 or 128 (the same for all), and up to 14 MB.  fp32 arithmetic, sums in a fixed order: a step is bit-reproducible.  Errors of the sums, about 2^-24 of
  * |u|_F, grow with the smallest singular values, by up to a^steps.  May be captured into a HIP graph, after an eager call
  * of as many steps. */
 #define QALORA_MUON_MAX_TENSORS 32

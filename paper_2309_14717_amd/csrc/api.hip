@@ -1171,6 +1171,18 @@ int qalora_muon_step(const qalora_muon* hp, int n_tensors, float* const* params,
                                                                      : 1.0;
     t.t[i].step_size = (float)((double)hp->lr * scale);
   }
+  // Matrices are worked on side by side: one that lies in another would be read while it is written.
+  struct Run {
+    uintptr_t begin, end;
+  } run[3 * MUON_MAX_TENSORS];
+  for (int i = 0; i < n_tensors; ++i) {
+    const size_t bytes = (size_t)rows[i] * cols[i] * sizeof(float);
+    const float* of[3] = {params[i], grads[i], momentum[i]};
+    for (int k = 0; k < 3; ++k) run[3 * i + k] = {reinterpret_cast<uintptr_t>(of[k]), reinterpret_cast<uintptr_t>(of[k]) + bytes};
+  }
+  std::sort(run, run + 3 * n_tensors, [](const Run& x, const Run& y) { return x.begin < y.begin; });
+  for (int i = 1; i < 3 * n_tensors; ++i)
+    if (run[i].begin < run[i - 1].end) return QALORA_EINVAL;
   if (misaligned(ws)) return QALORA_EALIGN;
   if (!ws || ws_bytes < floats * sizeof(float)) return QALORA_EWORKSPACE;
   MuonHyper h{};

@@ -90,14 +90,20 @@ def test_argument_errors_are_caught_before_launch():
     assert lib.qalora_muon_workspace_bytes(2, I2(16, 129), I2(400, 129)) == 0
     assert lib.qalora_muon_workspace_bytes(0, rows, cols) == lib.qalora_muon_workspace_bytes(2, None, cols) == 0
     good, odd, none = P2(0x10000, 0x20000), P2(0x10000, 0x20004), P2(0x10000, None)
+    G, M = P2(0x30000, 0x40000), P2(0x50000, 0x60000)
     W = ctypes.c_void_p(0x100000)
 
-    def call(hp=api.Muon(lr=0.1), n=2, p=good, g=good, m=good, r=rows, c=cols, ws=W, nbytes=size):
+    def call(hp=api.Muon(lr=0.1), n=2, p=good, g=G, m=M, r=rows, c=cols, ws=W, nbytes=size):
         return lib.qalora_muon_step(ctypes.byref(hp) if hp else None, n, p, g, m, r, c, 0, ws, nbytes, None)
 
     for bad in (dict(hp=None), dict(p=None), dict(g=None), dict(m=None), dict(r=None), dict(c=None), dict(n=0), dict(n=33),
                 dict(p=none), dict(g=none), dict(m=none), dict(r=I2(0, 8))):
         assert call(**bad) == api.EINVAL, bad
+    end = 0x10000 + 4 * 16 * 400
+    for bad in (dict(p=P2(0x10000, 0x10000)), dict(g=good), dict(m=good), dict(m=G), dict(p=P2(0x10000, 0x10010)),
+                dict(g=P2(0x30000, end - 16)), dict(m=P2(0x20000 + 4 * 64 * 8 - 16, 0x70000))):
+        assert call(**bad) == api.EINVAL, bad        # matrices that overlap
+    assert call(p=P2(0x10000, end), ws=None) == api.EWORKSPACE   # neighbours do not
     nan, inf = float("nan"), float("inf")
     for hp in (dict(lr=-1.0), dict(lr=nan), dict(momentum=1.0), dict(momentum=-0.1), dict(momentum=nan), dict(eps=0.0),
                dict(eps=nan), dict(weight_decay=-1.0), dict(steps=0), dict(steps=17), dict(scale_mode=3), dict(scale_mode=-1),
