@@ -267,7 +267,7 @@ int qalora_forward_deployed_epilogue(const qalora_desc* desc, int tokens, const 
 
 /* Backward of the epilogue, at the z the forward kept:
  *   dz = dy * mul * act'(z);   dmul = dy * act(z);   dbias = sum over the tokens of dz      (d residual = dy).
- * dz is the dy of qalora_backward.  All [tokens, cols], cols a multiple of 8 (QALORA_EUNSUPPORTED otherwise); arithmetic in
+ * dz is the dy of qalora_backward.  All [tokens, cols], cols a multiple of 8 up to 2^29 (QALORA_EUNSUPPORTED otherwise); arithmetic in
  * fp32, dz and dmul rounded to bf16, dbias the sum of the unrounded values.
  * in : dy fp32 or bf16 per dy_dtype; z bf16, NULL allowed where neither act nor dmul needs it; mul bf16 or NULL
  * out: dz, dmul bf16, dbias fp32 [cols]: at least one, the others NULL; dmul only with mul; a bf16 dz may be dy itself.

@@ -671,7 +671,7 @@ int qalora_forward_epilogue(const qalora_desc* d, int tokens, const void* x, con
 }
 
 size_t qalora_epilogue_backward_workspace_bytes(int tokens, int cols) {
-  if (tokens <= 0 || cols <= 0 || cols % 8 != 0) return 0;
+  if (tokens <= 0 || cols <= 0 || cols % 8 != 0 || cols > EB_MAX_COLS) return 0;
   return align_up(epilogue_back_floats(tokens, cols) * sizeof(float));
 }
 
@@ -686,7 +686,7 @@ int qalora_epilogue_backward(int act, int tokens, int cols, const void* dy, int 
   if (misaligned(dy) || misaligned(z) || misaligned(mul) || misaligned(dz) || misaligned(dmul) || misaligned(dbias) ||
       misaligned(ws))
     return QALORA_EALIGN;
-  if (cols % 8 != 0) return QALORA_EUNSUPPORTED;
+  if (cols % 8 != 0 || cols > EB_MAX_COLS) return QALORA_EUNSUPPORTED;
   const size_t need = dbias ? epilogue_back_floats(tokens, cols) * sizeof(float) : 0;
   if (need > 0 && (!ws || ws_bytes < need)) return QALORA_EWORKSPACE;
   EpilogueBackArgs a{};

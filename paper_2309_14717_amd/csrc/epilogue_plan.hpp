@@ -8,6 +8,7 @@ constexpr int EB_THREADS = 256;
 constexpr int EB_MAX_LANES = 64;  // of eight columns each: a row of a block's tile is up to 1 KB of bf16
 constexpr int EB_MIN_LANES = 8;   // 128 bytes
 constexpr int EB_ONE_BLOCK_ROWS = 256;
+constexpr int EB_MAX_COLS = 1 << 29;  // a launch has at most 2^32 threads, and narrow tiles take four to a column
 
 struct EpilogueBackPlan {
   int lanes;       // threads along a row (a power of two); the block takes EB_THREADS / lanes rows at a time

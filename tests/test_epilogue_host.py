@@ -104,6 +104,7 @@ def test_argument_errors_are_caught_before_launch():
         assert back(**bad) == api.EINVAL, bad
     for name in ("dy", "z", "mul", "dz", "dbias", "ws"):
         assert back(**{name: odd}) == api.EALIGN, name
-    assert back(cols=60) == api.EUNSUPPORTED
+    assert back(cols=60) == back(cols=2 ** 29 + 8) == api.EUNSUPPORTED
     assert back(T=300, dbias=good) == back(T=300, dbias=good, ws=good, n=64) == api.EWORKSPACE
     assert lib.qalora_epilogue_backward_workspace_bytes(0, 64) == lib.qalora_epilogue_backward_workspace_bytes(4, 60) == 0
+    assert lib.qalora_epilogue_backward_workspace_bytes(4, 2 ** 29 + 8) == 0

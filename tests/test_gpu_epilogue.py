@@ -195,6 +195,14 @@ def test_backward_forms(gpu_api):
     assert torch.equal(gpu_api.epilogue_backward(dy, mul=mul, z=z)[1], (dy.float() * z.float()).to(BF16))
 
 
+def test_backward_of_one_row_of_many_columns(gpu_api):
+    """As many columns as are taken, 2^29: the launch has 2^31 threads."""
+    cols = 2 ** 29
+    dy = torch.randn(1 << 20, device="cuda").to(BF16).repeat(512).view(1, cols)
+    dz, none, db = gpu_api.epilogue_backward(dy, want_dbias=True)
+    assert none is None and torch.equal(dz, dy) and torch.equal(db.to(BF16), dy[0])
+
+
 @pytest.mark.parametrize("act", ec.ACTS)
 def test_gradients_against_differences(gpu_api, act):
     """dbias and the bias's differences in sum(dy * y), on a layer whose sums are exact.  A difference over +-h is off by h^2 / 6 of
