@@ -244,7 +244,7 @@ int qalora_backward_kept(const qalora_desc* desc, int tokens, const void* dy, co
  *   bias      fp32 [d_out]
  *   mul       bf16 [tokens, d_out]: with the up projection here, the gate's call gives a SwiGLU block's hidden activations
  *   residual  [tokens, d_out] of y's type; it may be y itself (the residual stream is then updated in place)
- *   z         out, bf16 [tokens, d_out]: z rounded, for qalora_epilogue_backward
+ *   z         out, bf16 [tokens, d_out]: z rounded, for qalora_epilogue_backward; not y, mul or residual
  * qalora_forward_epilogue is qalora_forward with it, or, where kept is not NULL, qalora_forward_keep;
  * qalora_forward_deployed_epilogue is qalora_forward_deployed with it.  Same kernels, workspaces, precision of
  * the product (few tokens: exact operands), limits and status word: y is what the epilogue makes of the sums that these calls

@@ -387,6 +387,9 @@ def forward_epilogue(desc: Desc, x, packed, alpha, beta, A=None, B=None, bias=No
     if y is None:
         y = torch.empty((T, desc.d_out), dtype=out_dtype, device=dev)
     _need_out(y, "y", T, desc.d_out, dev)
+    for t, wanted, name, flag in ((z, keep_z, "z", "keep_z"), (kept, keep, "kept", "keep")):
+        if t is not None and not wanted:
+            raise ValueError(f"{name}: given without {flag}")
     if keep_z and z is None:
         z = torch.empty((T, desc.d_out), dtype=torch.bfloat16, device=dev)
     if keep:

@@ -644,9 +644,10 @@ static int forward_impl(const qalora_desc* d, int tokens, const void* x, const v
 }
 
 // The header's epilogue as the kernels take it; null: none.
-static int read_epilogue(const qalora_epilogue* from, Epilogue& e, const Epilogue** use) {
+static int read_epilogue(const qalora_epilogue* from, const void* y, Epilogue& e, const Epilogue** use) {
   *use = nullptr;
   if (!from) return QALORA_OK;
+  if (from->z && (from->z == y || from->z == from->mul || from->z == from->residual)) return QALORA_EINVAL;  // z is stored first
   if (from->act < QALORA_ACT_NONE || from->act > QALORA_ACT_GELU_TANH) return QALORA_EINVAL;
   if (misaligned(from->bias) || misaligned(from->mul) || misaligned(from->residual) || misaligned(from->z)) return QALORA_EALIGN;
   e.bias = from->bias;
@@ -665,7 +666,7 @@ int qalora_forward_epilogue(const qalora_desc* d, int tokens, const void* x, con
   if ((A == nullptr) != (B == nullptr)) return QALORA_EINVAL;
   Epilogue e{};
   const Epilogue* use;
-  if (const int rc = read_epilogue(epilogue, e, &use); rc != QALORA_OK) return rc;
+  if (const int rc = read_epilogue(epilogue, y, e, &use); rc != QALORA_OK) return rc;
   return forward_impl(d, tokens, x, packed, alpha, beta, single_part(d, A, B, nullptr, nullptr), y, y_dtype, kept,
                       kept != nullptr, ws, ws_bytes, stream, nullptr, use);
 }
@@ -681,7 +682,7 @@ int qalora_epilogue_backward(int act, int tokens, int cols, const void* dy, int 
   if (dy_dtype != QALORA_F32 && dy_dtype != QALORA_BF16) return QALORA_EINVAL;
   if (accumulate != 0 && accumulate != 1) return QALORA_EINVAL;
   if (!dz && !dmul && !dbias) return QALORA_EINVAL;
-  if (dmul && !mul) return QALORA_EINVAL;
+  if (dmul && (!mul || dmul == dz)) return QALORA_EINVAL;
   if (!z && (act != QALORA_ACT_NONE || dmul)) return QALORA_EINVAL;
   if (misaligned(dy) || misaligned(z) || misaligned(mul) || misaligned(dz) || misaligned(dmul) || misaligned(dbias) ||
       misaligned(ws))
@@ -995,7 +996,7 @@ int qalora_forward_deployed_epilogue(const qalora_desc* d, int tokens, const voi
                                      void* ws, size_t ws_bytes, void* stream) {
   Epilogue e{};
   const Epilogue* use;
-  if (const int rc = read_epilogue(epilogue, e, &use); rc != QALORA_OK) return rc;
+  if (const int rc = read_epilogue(epilogue, y, e, &use); rc != QALORA_OK) return rc;
   return forward_deployed_impl(d, tokens, x, packed, deployed, y, y_dtype, ws, ws_bytes, stream, use);
 }
 

@@ -633,7 +633,7 @@ FASTCALL(forward_epilogue, 18)
   Weights w = weights(c, a[2], a[3], a[4]);
   adapter(c, a[5], a[6], w);
   const bool keep_z = c.truth(a[11]), keep = c.truth(a[12]);
-  c.need(!keep || w.A);
+  c.need((!keep || w.A) && (keep_z || a[16] == Py_None) && (keep || a[17] == Py_None));
   int code = 0;
   const at::Tensor y = c.out(a[15], a[13], c.T, c.desc.d_out, code);
   qalora_epilogue e = epilogue(c, a[7], a[8], a[9], a[10], code);

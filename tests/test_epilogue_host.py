@@ -84,6 +84,9 @@ def test_argument_errors_are_caught_before_launch():
         assert forward(**bad) == api.EINVAL, bad
     for k, name in enumerate(("bias", "mul", "residual", "z")):
         assert forward(epi=api.Epilogue(1, **{name: 0x10008})) == api.EALIGN, name
+    for name in ("mul", "residual"):
+        assert forward(epi=api.Epilogue(1, z=0x20000, **{name: 0x20000})) == api.EINVAL, name
+    assert forward(epi=api.Epilogue(0, z=0x10000)) == api.EINVAL       # y
     assert forward(x=odd) == forward(y=odd) == api.EALIGN
     for epi in (None, api.Epilogue(2, bias=0x10000)):
         assert forward(epi=epi, n=64) == forward(epi=epi, ws=None) == api.EWORKSPACE
@@ -100,7 +103,7 @@ def test_argument_errors_are_caught_before_launch():
         return lib.qalora_epilogue_backward(act, T, cols, dy, dt, z, mul, dz, dmul, dbias, acc, ws, n, None)
 
     for bad in (dict(act=-1), dict(act=5), dict(T=0), dict(cols=0), dict(dy=None), dict(dt=2), dict(dz=None), dict(z=None),
-                dict(acc=2), dict(dmul=good), dict(act=0, z=None, mul=good, dmul=good)):
+                dict(acc=2), dict(dmul=good), dict(mul=good, dmul=good), dict(act=0, z=None, mul=good, dmul=good)):
         assert back(**bad) == api.EINVAL, bad
     for name in ("dy", "z", "mul", "dz", "dbias", "ws"):
         assert back(**{name: odd}) == api.EALIGN, name

@@ -291,6 +291,10 @@ def test_refusals(gpu_api):
         layer.call(act="tanh")
     with pytest.raises(ValueError, match="z: dtype"):
         layer.call(z=torch.zeros((T, n), device="cuda"), keep_z=True)
+    with pytest.raises(ValueError, match="z: given"):
+        layer.call(z=torch.zeros((T, n), device="cuda", dtype=BF16))
+    with pytest.raises(ValueError, match="kept: given"):
+        layer.call(kept=torch.zeros(4096, device="cuda", dtype=torch.uint8))
     with pytest.raises(gpu_api.QaloraError):
         layer.call(keep=True)                # nothing to keep without an adapter
     dy = torch.zeros((T, n), device="cuda", dtype=BF16)
