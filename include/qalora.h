@@ -423,7 +423,8 @@ int qalora_adamw_step(const qalora_adamw* hp, int step, int n_tensors, float* co
  * params and momentum are updated in place; grads are read, and set to zero afterwards if zero_grads != 0.
  * rows, cols: HOST arrays.  The shorter side is at most QALORA_MUON_MAX_SHORT (the rank of an adapter;
  * QALORA_EUNSUPPORTED otherwise), the longer one at most 2^27.  eps > 0; a matrix of zeros gets the update zero.
- * A matrix with an infinity or a NaN in u becomes NaN, the others do not see it.
+ * A matrix with an infinity or a NaN in u, or |u|_F above 1.8e19, becomes NaN, the others do not see it.  |u|_F below 2^-47 counts
+ * as 2^-47 in X0.
  * ws: qalora_muon_workspace_bytes(n_tensors, rows, cols) bytes (0 for a list that is not acceptable): what the matrices take
  * themselves with every shorter side padded to 32, 64 or 128 (the same for all), and up to 14 MB.  fp32 arithmetic, sums in a fixed order: a step is bit-reproducible.  Errors of the sums, about 2^-24 of
  * |u|_F, grow with the smallest singular values, by up to a^steps.  May be captured into a HIP graph, after an eager call

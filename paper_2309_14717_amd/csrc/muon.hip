@@ -350,8 +350,11 @@ struct Scales {
   float p, y;          // of P and of P X (once P is there)
   float trace, x_bound;
   __device__ __forceinline__ Scales(float trace_, float eps, bool first) {
-    x_norm = first ? 1.0f / (__fsqrt_rn(trace_) + eps) : 1.0f;
-    x_bound = (__fsqrt_rn(trace_) + kLostNorm) * x_norm;
+    // (A norm that squares lost below the smallest fp32 may miss counts as that much: with a small eps, X0 could be of any size.
+    // A comparison, which keeps a NaN.)
+    const float norm = __fsqrt_rn(trace_);
+    x_norm = first ? 1.0f / ((norm < kLostNorm ? kLostNorm : norm) + eps) : 1.0f;
+    x_bound = (norm + kLostNorm) * x_norm;
     trace = trace_ * x_norm * x_norm;
     g = scale_below(trace);
     x = scale_below(x_bound);

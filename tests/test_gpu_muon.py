@@ -246,6 +246,25 @@ def test_refusals(gpu_api):
     assert not ok[0].any()
 
 
+@pytest.mark.parametrize("kind", sorted(KINDS))
+@pytest.mark.parametrize("eps", [1e-30, 1e-37])
+def test_lost_norms_with_a_tiny_eps(gpu_api, eps, kind):
+    """Zeros, and gradients whose squares are lost in fp32: X0 is their multiple by 2^47 at most, far below one, and every pass
+    multiplies it by a: the update is a^steps X0.  Tolerance: the first pass takes X0 for a matrix of norm one, times 2^14 in two fp16
+    whose lower one has steps of 2^-24: off by half of that, 2^-39 an element, at most; and 32 * 2^-24 a pass, as above."""
+    rng = np.random.default_rng(15)
+    shapes = [(16, 300), (300, 20), KINDS[kind], (12, 40)]
+    g = [gradient(rng, *s, kind="noise") * np.float32(1e-20) for s in shapes]
+    g[3][:] = 0
+    hp = gpu_api.Muon(lr=1.0, momentum=0.0, eps=eps, nesterov=False, scale_mode=0)
+    dp, dg, dm = up([np.zeros(s, np.float32) for s in shapes]), up(g), up([np.zeros(s, np.float32) for s in shapes])
+    gpu_api.muon_step(hp, dp, dg, dm)
+    for i in range(len(shapes)):
+        X0 = 2.0 ** 47 * g[i].astype(np.float64)
+        off = np.linalg.norm(-dp[i].cpu().numpy().astype(np.float64) - A ** 5 * X0)
+        assert off <= A ** 5 * (2.0 ** -39 * X0.size ** 0.5 + 5 * 32 * 2.0 ** -24 * np.linalg.norm(X0))
+
+
 @pytest.mark.parametrize("size", [1e-15, 1e-8, 1.0, 1e8, 1e15])
 def test_gradients_of_any_size(gpu_api, size):
     """The direction does not depend on the gradients' size (eps far below them)."""
