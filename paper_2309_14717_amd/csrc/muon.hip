@@ -250,38 +250,41 @@ struct Elements {
 
 constexpr int muon_waves(int rt) { return muon_waves_of(rt); }  // of a block: 512 registers each, or 256
 
-// The wavefronts' G tiles (upper ones, in results' layout) added in order; the sum is the first wavefront's.
-template <int RT>
-__device__ __forceinline__ void add_shares(f32x16 (&g)[muon_upper(RT)], f32x4* lds, int wave, int lane) {
-  constexpr int NW = muon_waves(RT), U = muon_upper(RT);
+// The wavefronts' G tiles (upper ones, in results' layout) added in order through LDS, some tiles at a time:
+// sink(tile, quad, lane, sum), from the whole block.
+constexpr int muon_tiles_at_once(int rt) { return rt > 2 ? muon_upper(rt) / 2 : muon_upper(rt); }
+template <int RT, typename Sink>
+__device__ __forceinline__ void add_shares(const f32x16 (&g)[muon_upper(RT)], f32x4* lds, int wave, int lane, Sink&& sink) {
+  constexpr int NW = muon_waves(RT), U = muon_upper(RT), AT_ONCE = muon_tiles_at_once(RT);
+  static_assert(U % AT_ONCE == 0, "whole batches");
 #pragma unroll
-  for (int half = NW / 2; half >= 1; half /= 2) {  // the upper half of the wavefronts to the lower one
+  for (int u0 = 0; u0 < U; u0 += AT_ONCE) {
     __syncthreads();
-    if (wave >= half && wave < 2 * half)
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+    for (int u = 0; u < AT_ONCE; ++u)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) lds[(((wave - half) * U + u) * 4 + q) * 64 + lane] = quad_of(g[u], q);
+      for (int q = 0; q < 4; ++q) lds[((wave * AT_ONCE + u) * 4 + q) * 64 + lane] = quad_of(g[u0 + u], q);
     __syncthreads();
-    if (wave < half)
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+    for (int k = 0; k < (AT_ONCE * 4 + NW - 1) / NW; ++k) {
+      const int piece = wave + NW * k;  // tile and quad: 64 pieces of 16 bytes
+      if (piece >= AT_ONCE * 4) break;
+      f32x4 v = lds[piece * 64 + lane];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const f32x4 v = lds[((wave * U + u) * 4 + q) * 64 + lane];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) g[u][4 * q + e] += v[e];
-        }
+      for (int w = 1; w < NW; ++w) v += lds[(w * AT_ONCE * 4 + piece) * 64 + lane];
+      sink(u0 + (piece >> 2), piece & 3, lane, v);
+    }
   }
 }
 template <int RT>
-__device__ __forceinline__ void store_share(f32x16 (&g)[muon_upper(RT)], f32x4* lds, f32x4* out, int wave, int lane) {
-  add_shares<RT>(g, lds, wave, lane);
-  if (wave == 0)
-#pragma unroll
-    for (int u = 0; u < muon_upper(RT); ++u)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) out[(u * 4 + q) * 64 + lane] = quad_of(g[u], q);
+__device__ __forceinline__ void store_share(const f32x16 (&g)[muon_upper(RT)], f32x4* lds, f32x4* out, int wave, int lane) {
+  add_shares<RT>(g, lds, wave, lane, [&](int u, int q, int l, const f32x4& v) { out[(u * 4 + q) * 64 + l] = v; });
+}
+// Row and column of the upper tile u.
+__device__ __forceinline__ void upper_tile(int u, int& a, int& b) {
+  b = 0;
+  while ((b + 1) * (b + 2) / 2 <= u) ++b;
+  a = u - b * (b + 1) / 2;
 }
 // Quad q of G's tile (a, b) and, off the diagonal, its mirror image: element (8 q + 4 (lane / 32) + k, lane % 32) at its place.
 template <int RT>
@@ -295,7 +298,7 @@ __device__ __forceinline__ void put_gram(float* gram, int a, int b, int q, int l
     gram[(b * RT + a) * 1024 + ((col >> 3) * 64 + row + 32 * ((col >> 2) & 1)) * 4 + (col & 3)] = v[k];
   }
 }
-constexpr size_t muon_share_lds(int rt) { return (size_t)muon_waves(rt) / 2 * muon_upper(rt) * 4096; }
+constexpr size_t muon_share_lds(int rt) { return (size_t)muon_waves(rt) * muon_tiles_at_once(rt) * 4096; }
 constexpr size_t muon_p_lds(int rt) { return (size_t)rt * rt * 4096; }
 constexpr size_t muon_turn_lds(int rt) { return muon_waves(rt) * muon_turn_floats(rt) * 4; }
 constexpr size_t muon_start_lds(int rt) { return std::max(muon_share_lds(rt), muon_turn_lds(rt)); }
@@ -616,11 +619,9 @@ __global__ __launch_bounds__(256) void muon_reduce_kernel(const MuonTable table,
   if (group > 0) return;
 #pragma unroll
   for (int k = 1; k < 8; ++k) v += part[k][e];
-  const int u = at >> 8, q = (at >> 6) & 3, lane = at & 63;
-  int b = 0;
-  while ((b + 1) * (b + 2) / 2 <= u) ++b;
-  const int a = u - b * (b + 1) / 2;
-  put_gram<RT>(ws + t.gram, a, b, q, lane, v);
+  int a, b;
+  upper_tile(at >> 8, a, b);
+  put_gram<RT>(ws + t.gram, a, b, (at >> 6) & 3, at & 63, v);
 }
 
 // One step of the iteration.  first: X holds u, whose norm comes off here.
@@ -659,14 +660,11 @@ __global__ __launch_bounds__(64 * muon_waves(RT), 1) void muon_alone_kernel(cons
   auto next_p = [&](bool first) {
     int lane = w.lane;
     asm volatile("" : "+v"(lane));  // (else the places in LDS that depend on it are held in registers throughout)
-    add_shares<RT>(g, shares, w.wave, lane);
-    if (w.wave == 0)
-#pragma unroll
-      for (int b = 0; b < RT; ++b)
-#pragma unroll
-        for (int a = 0; a <= b; ++a)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) put_gram<RT>(gram, a, b, q, lane, quad_of(g[upper_at(a, b)], q));
+    add_shares<RT>(g, shares, w.wave, lane, [&](int u, int q, int l, const f32x4& v) {
+      int a, b;
+      upper_tile(u, a, b);
+      put_gram<RT>(gram, a, b, q, l, v);
+    });
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < 4 * RT; ++q) coming[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
