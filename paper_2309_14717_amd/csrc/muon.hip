@@ -125,13 +125,23 @@ __device__ __forceinline__ void turn(const Operand (&in)[2], const f16x8 (&unit)
 constexpr int muon_upper(int tiles) { return muon_upper_tiles(tiles); }
 constexpr int upper_at(int a, int b) { return b * (b + 1) / 2 + a; }
 
-// The tensor whose blocks the launch's block lies in.  (All starts are compared at once: a search that reads one after
-// the other waits for each, 0.15 us a tensor.)
-__device__ __forceinline__ int muon_find(const int (&first)[MUON_MAX_TENSORS]) {
-  int ti = 0;
+// The tensor whose blocks the launch's block lies in, and the block's number in it.  A lane reads each tensor's first block and entry, and
+// the right one's words are handed round: one wait for memory, where a search and then its entry are two (0.5 us, in every
+// launch).
+__device__ __forceinline__ MuonTensor muon_find(const MuonTable& table, const int (&first)[MUON_MAX_TENSORS], int& number) {
+  constexpr int WORDS = sizeof(MuonTensor) / 4;
+  static_assert(MUON_MAX_TENSORS == 32 && sizeof(MuonTensor) % 4 == 0, "a lane for each");
+  struct Words {
+    int w[WORDS];
+  };
+  const int mine = threadIdx.x & 31;
+  const int begin = first[mine];
+  Words e = __builtin_bit_cast(Words, table.t[mine]);
+  const int ti = __builtin_popcount((uint32_t)__ballot((int)blockIdx.x >= begin)) - 1;
+  number = (int)blockIdx.x - __builtin_amdgcn_readlane(begin, ti);
 #pragma unroll
-  for (int i = 1; i < MUON_MAX_TENSORS; ++i) ti += (int)blockIdx.x >= first[i] ? 1 : 0;
-  return ti;
+  for (int k = 0; k < WORDS; ++k) e.w[k] = __builtin_amdgcn_readlane(e.w[k], ti);
+  return __builtin_bit_cast(MuonTensor, e);
 }
 
 // Reads or writes the lane's elements of 32 columns of X, from column n0 on, in a [rows, cols] matrix.
@@ -590,8 +600,8 @@ __device__ __forceinline__ void pass_columns(const Columns<RT>& w, const MuonHyp
 template <int RT>
 __global__ __launch_bounds__(64 * muon_waves(RT), 1) void muon_start_kernel(const MuonTable table, const MuonHyper h, float* ws) {
   extern __shared__ __align__(16) f32x4 lds[];
-  const int ti = muon_find(table.block0), slice = (int)blockIdx.x - table.block0[ti];
-  const MuonTensor& t = table.t[ti];
+  int slice;
+  const MuonTensor t = muon_find(table, table.block0, slice);
   const Columns<RT> w(t, ws, slice * table.per_block, min(t.chunks, (slice + 1) * table.per_block), reinterpret_cast<float*>(lds));
   f32x16 g[muon_upper(RT)];
   start_columns<RT>(w, h, g);
@@ -603,12 +613,12 @@ __global__ __launch_bounds__(64 * muon_waves(RT), 1) void muon_start_kernel(cons
 template <int RT>
 __global__ __launch_bounds__(256) void muon_reduce_kernel(const MuonTable table, float* ws) {
   __shared__ f32x4 part[8][32];
-  const int ti = muon_find(table.reduce0);
-  const MuonTensor& t = table.t[ti];
+  int number;
+  const MuonTensor t = muon_find(table, table.reduce0, number);
   const int slices = (t.chunks + table.per_block - 1) / table.per_block;
   const int e = threadIdx.x & 31, group = threadIdx.x >> 5;
   constexpr int pieces = muon_upper(RT) * 256;
-  const int at = (int)(blockIdx.x - table.reduce0[ti]) * 32 + e;
+  const int at = number * 32 + e;
   const f32x4* src = reinterpret_cast<const f32x4*>(ws + t.partial) + at;
   const int per = (slices + 7) / 8, z0 = min(slices, group * per), z1 = min(slices, z0 + per);
   f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -629,8 +639,8 @@ template <int RT, bool LAST>
 __global__ __launch_bounds__(64 * muon_waves(RT), 1) void muon_pass_kernel(const MuonTable table, const MuonHyper h, bool first, float* ws) {
   extern __shared__ __align__(16) f32x4 lds[];
   __shared__ float squares[muon_waves(RT)];
-  const int ti = muon_find(table.block0), slice = (int)blockIdx.x - table.block0[ti];
-  const MuonTensor& t = table.t[ti];
+  int slice;
+  const MuonTensor t = muon_find(table, table.block0, slice);
   const Columns<RT> w(t, ws, slice * table.per_block, min(t.chunks, (slice + 1) * table.per_block),
                       reinterpret_cast<float*>(lds) + muon_p_lds(RT) / 4);
   // The columns that come next are on their way: the first ones while P is made, later ones while those before are worked on.
