@@ -121,6 +121,28 @@ __device__ __forceinline__ void turn(const Operand (&in)[2], const f16x8 (&unit)
   for (int s = 0; s < 2; ++s) out[s] = Operand{to_half(hi, 8 * s), to_half(lo, 8 * s)};
 }
 
+// op over the wavefront, in every lane, between neighbours, quads, eights, rows of 16 and halves.  (Lane by lane through LDS, as
+// __shfl_xor goes, six steps are 0.4 us, and each pass waits for two sums.)
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+template <typename Op>
+__device__ __forceinline__ float over_wave(float v, Op&& op) {
+  v = op(v, moved<0xb1>(v));   // lane ^ 1
+  v = op(v, moved<0x4e>(v));   // lane ^ 2
+  v = op(v, moved<0x141>(v));  // 7 - lane of eight
+  v = op(v, moved<0x140>(v));  // 15 - lane of sixteen
+  uint32_t w = __float_as_uint(v);
+  const auto row = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+  w = __float_as_uint(op(__uint_as_float(row[0]), __uint_as_float(row[1])));
+  const auto half = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+  return op(__uint_as_float(half[0]), __uint_as_float(half[1]));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  return over_wave(v, [](float x, float y) { return x + y; });
+}
+
 // The upper tiles of a symmetric RT x RT matrix of tiles in the order (0,0), (0,1), (1,1), (0,2), ...
 constexpr int muon_upper(int tiles) { return muon_upper_tiles(tiles); }
 constexpr int upper_at(int a, int b) { return b * (b + 1) / 2 + a; }
@@ -352,9 +374,7 @@ __device__ __forceinline__ float momentum_step(const MuonTensor& t, const MuonHy
     for (int q = 0; q < 4 * RT; ++q) zero[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     at.store(t.g, zero);
   }
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, 64));
-  return most;
+  return over_wave(most, [](float x, float y) { return fmaxf(x, y); });
 }
 
 // The scales of a pass and the norm that comes off X in the first one.
@@ -386,11 +406,6 @@ __device__ __forceinline__ void put_operands(f32x4* lds, int tile, int lane, con
 __device__ __forceinline__ Operand operand_at(const f32x4* lds, int tile, int s, int lane) {
   const f32x4* at = lds + (2 * tile + s) * 128 + lane;
   return Operand{__builtin_bit_cast(f16x8, at[0]), __builtin_bit_cast(f16x8, at[64])};
-}
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
-  return v;
 }
 
 // The chunks of a wavefront: every muon_waves-th of its block's.
