@@ -121,6 +121,10 @@ __device__ __forceinline__ void turn(const Operand (&in)[2], const f16x8 (&unit)
   for (int s = 0; s < 2; ++s) out[s] = Operand{to_half(hi, 8 * s), to_half(lo, 8 * s)};
 }
 
+// A barrier for what goes through LDS: loads of coming columns stay in flight, and stores of X (which its own wavefront reads again)
+// are not waited for.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // op over the wavefront, in every lane, between neighbours, quads, eights, rows of 16 and halves.  (Lane by lane through LDS, as
 // __shfl_xor goes, six steps are 0.4 us, and each pass waits for two sums.)
 template <int CTRL>
@@ -291,12 +295,12 @@ __device__ __forceinline__ void add_shares(const f32x16 (&g)[muon_upper(RT)], f3
   static_assert(U % AT_ONCE == 0, "whole batches");
 #pragma unroll
   for (int u0 = 0; u0 < U; u0 += AT_ONCE) {
-    __syncthreads();
+    lds_barrier();
 #pragma unroll
     for (int u = 0; u < AT_ONCE; ++u)
 #pragma unroll
       for (int q = 0; q < 4; ++q) lds[((wave * AT_ONCE + u) * 4 + q) * 64 + lane] = quad_of(g[u0 + u], q);
-    __syncthreads();
+    lds_barrier();
 #pragma unroll
     for (int k = 0; k < (AT_ONCE * 4 + NW - 1) / NW; ++k) {
       const int piece = wave + NW * k;  // tile and quad: 64 pieces of 16 bytes
@@ -412,21 +416,24 @@ __device__ __forceinline__ Operand operand_at(const f32x4* lds, int tile, int s,
 template <int RT>
 struct Columns {
   const MuonTensor& t;
-  f32x4* x;     // the lane's place in X
+  f32x4* x;     // X
   int first, end;
   int wave, lane;
   float* room;  // the wavefront's, for tall matrices
   __device__ __forceinline__ Columns(const MuonTensor& t_, float* ws, int begin, int end_, float* rooms)
       : t(t_), end(end_), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63) {
     first = begin + wave;
-    x = reinterpret_cast<f32x4*>(ws + t.x) + lane;
+    x = reinterpret_cast<f32x4*>(ws + t.x);
     room = rooms + wave * muon_turn_floats(RT);
   }
-  __device__ __forceinline__ f32x4* at(int c) const { return x + (size_t)c * RT * 256; }
+  __device__ __forceinline__ f32x4* at(int c) const { return x + (size_t)c * RT * 256 + lane; }
+  // (No branch for a chunk beyond the last: behind one, a wait for what was requested before takes these loads for absent and
+  // waits for them too.  The buffer is empty instead.)
   __device__ __forceinline__ void request(int c, f32x4 (&coming)[4 * RT]) const {
-    if (c < end)
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(x + (size_t)c * RT * 256, 0, c < end ? RT * 4096 : 0, 0x00020000);
 #pragma unroll
-      for (int q = 0; q < 4 * RT; ++q) coming[q] = at(c)[64 * q];
+    for (int q = 0; q < 4 * RT; ++q)
+      coming[q] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * lane + 1024 * q, 0, 0));
   }
 };
 
@@ -462,24 +469,31 @@ __device__ __forceinline__ void start_columns(const Columns<RT>& w, const MuonHy
   }
 }
 
-// P = a I + b G + c G^2 as operands in LDS, its tile (t, a) at a RT + t (G's were there before).
-template <int RT>
-__device__ __forceinline__ Scales make_p(const float* gram, const MuonHyper& h, bool first, f32x4* lds, float* squares, int wave, int lane) {
+// P = a I + b G + c G^2 as operands in LDS, its tile (t, a) at a RT + t (G's were there before).  meanwhile() requests what is
+// needed after it: behind G's loads, whose wait would otherwise include it.
+template <int RT, typename Fn>
+__device__ __forceinline__ Scales make_p(const float* gram, const MuonHyper& h, bool first, f32x4* lds, float* squares, int wave, int lane, Fn&& meanwhile) {
   constexpr int NW = muon_waves(RT);
   // A wavefront has tiles (t, a) of G and of P, in results' layout: the operand for rows of tile a and slices of tile t.
   constexpr int PT = (RT * RT + NW - 1) / NW;
   f32x4 p[PT][4];
 #pragma unroll
-  for (int k = 0; k < PT; ++k)
-    if (wave + NW * k < RT * RT)
+  for (int k = 0; k < PT; ++k)  // (some wavefronts for nothing: no branch, see Columns::request)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) p[k][q] = reinterpret_cast<const f32x4*>(gram)[(wave + NW * k) * 256 + q * 64 + lane];
-  float diagonal = 0.0f;
+    for (int q = 0; q < 4; ++q) p[k][q] = reinterpret_cast<const f32x4*>(gram)[min(wave + NW * k, RT * RT - 1) * 256 + q * 64 + lane];
+  float ds[(32 * RT + 63) / 64];
 #pragma unroll
   for (int k = 0; k < (32 * RT + 63) / 64; ++k) {
-    const int d = lane + 64 * k, a = d >> 5, dd = d & 31;
-    if (d < 32 * RT) diagonal += gram[(a * RT + a) * 1024 + ((dd >> 3) * 64 + dd + 32 * ((dd >> 2) & 1)) * 4 + (dd & 3)];
+    const int d = lane + 64 * k, a = min(d >> 5, RT - 1), dd = d & 31;
+    const float on = gram[(a * RT + a) * 1024 + ((dd >> 3) * 64 + dd + 32 * ((dd >> 2) & 1)) * 4 + (dd & 3)];
+    ds[k] = d < 32 * RT ? on : 0.0f;
   }
+  __builtin_amdgcn_sched_barrier(0);
+  meanwhile();
+  __builtin_amdgcn_sched_barrier(0);
+  float diagonal = 0.0f;
+#pragma unroll
+  for (int k = 0; k < (32 * RT + 63) / 64; ++k) diagonal += ds[k];
   Scales s(wave_sum(diagonal), h.eps, first);
 #pragma unroll
   for (int k = 0; k < PT; ++k)
@@ -489,7 +503,7 @@ __device__ __forceinline__ Scales make_p(const float* gram, const MuonHyper& h, 
         p[k][q] *= s.x_norm * s.x_norm;
       put_operands(lds, wave + NW * k, lane, p[k], s.g);
     }
-  __syncthreads();
+  lds_barrier();
   float square = 0.0f;
   const float g_back = inverse_power(s.g) * inverse_power(s.g);
 #pragma unroll
@@ -512,7 +526,7 @@ __device__ __forceinline__ Scales make_p(const float* gram, const MuonHyper& h, 
     }
   square = wave_sum(square);
   if (lane == 0) squares[wave] = square;
-  __syncthreads();  // (also: G has been read, and its place is free)
+  lds_barrier();  // (also: G has been read, and its place is free)
   float p_bound = 0.0f;
 #pragma unroll
   for (int k = 0; k < NW; ++k) p_bound += squares[k];
@@ -522,7 +536,7 @@ __device__ __forceinline__ Scales make_p(const float* gram, const MuonHyper& h, 
 #pragma unroll
   for (int k = 0; k < PT; ++k)
     if (wave + NW * k < RT * RT) put_operands(lds, (wave + NW * k) % RT * RT + (wave + NW * k) / RT, lane, p[k], s.p);
-  __syncthreads();
+  lds_barrier();
   return s;
 }
 
@@ -660,10 +674,7 @@ __global__ __launch_bounds__(64 * muon_waves(RT), 1) void muon_pass_kernel(const
                       reinterpret_cast<float*>(lds) + muon_p_lds(RT) / 4);
   // The columns that come next are on their way: the first ones while P is made, later ones while those before are worked on.
   f32x4 coming[4 * RT];
-#pragma unroll
-  for (int q = 0; q < 4 * RT; ++q) coming[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  w.request(w.first, coming);
-  const Scales s = make_p<RT>(ws + t.gram, h, first, lds, squares, w.wave, w.lane);
+  const Scales s = make_p<RT>(ws + t.gram, h, first, lds, squares, w.wave, w.lane, [&] { w.request(w.first, coming); });
   f32x16 g[muon_upper(RT)];
   pass_columns<RT, LAST>(w, h, s, lds, coming, g);
   if constexpr (!LAST)
@@ -690,11 +701,8 @@ __global__ __launch_bounds__(64 * muon_waves(RT), 1) void muon_alone_kernel(cons
       upper_tile(u, a, b);
       put_gram<RT>(gram, a, b, q, l, v);
     });
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < 4 * RT; ++q) coming[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    w.request(w.first, coming);
-    return make_p<RT>(gram, h, first, lds, squares, w.wave, lane);
+    lds_barrier();
+    return make_p<RT>(gram, h, first, lds, squares, w.wave, lane, [&] { w.request(w.first, coming); });
   };
   for (int k = 0; k + 1 < steps; ++k) {
     const Scales s = next_p(k == 0);
