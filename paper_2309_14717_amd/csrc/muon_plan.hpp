@@ -36,7 +36,7 @@ constexpr int muon_upper_tiles(int tiles) { return tiles * (tiles + 1) / 2; }
 constexpr int muon_waves_of(int tiles) { return tiles > 2 ? 4 : 8; }
 constexpr int MUON_BLOCKS = 256;
 // One launch, a block for each matrix, where the longest has this many 32 x 32 tiles of X at most.  Two matrices, 5 steps, us (one
-// launch against eleven): 32 x 512 27 / 52, 1024 42 / 53, 2048 69 / 54; 64 x 512 53 / 70, 1024 84 / 71.
+// launch against eleven): 32 x 512 25 / 41, 1024 38 / 42, 1280 45 / 43; 64 x 512 48 / 56, 768 62 / 56; fourteen alike.
 constexpr int MUON_ALONE_TILES = 32;
 
 // Fills in the table from rows[] and cols[]; returns the workspace's floats, 0 where the list is not acceptable
