@@ -428,7 +428,7 @@ int qalora_adamw_step(const qalora_adamw* hp, int step, int n_tensors, float* co
  * ws: qalora_muon_workspace_bytes(n_tensors, rows, cols) bytes (0 for a list that is not acceptable): what the matrices take
  * themselves with every shorter side padded to 32, 64 or 128 (the same for all), and up to 14 MB.  fp32 arithmetic, sums in a fixed order: a step is bit-reproducible.  Errors of the sums, about 2^-24 of
  * |u|_F, grow with the smallest singular values, by up to a^steps.  May be captured into a HIP graph, after an eager call
- * of as many steps. */
+ * with the same list and steps.  (Which matrices are in a list decides how its sums are split: a matrix's last bits may differ in another list.) */
 #define QALORA_MUON_MAX_TENSORS 32
 #define QALORA_MUON_MAX_SHORT 128
 #define QALORA_MUON_MAX_STEPS 16

@@ -12,8 +12,8 @@
 // P = a I + b G + c G^2 (r^3 operations, repeated by every block, against r^2 per column of X), replaces its
 // columns of X by P X and adds the new columns' products to its own share of the next G; a small launch adds the shares in
 // block order (no atomics: a step is bit-reproducible).  X0's norm is the root of the first G's trace and goes into the first
-// pass, so the norm takes no pass of its own.  Small matrices (a block's work of a few microseconds a pass) take one launch, a block
-// each: the launches of a step are eleven with five passes.
+// pass, so the norm takes no pass of its own.  Where the shares are few, every block of a pass adds them by itself instead of a launch
+// between passes; small matrices take one launch for all, a block each.  Otherwise five passes are eleven launches.
 //
 // (G alone could carry the whole iteration: P is a polynomial in the first G.  But an error of 2^-24 in that G then meets
 // the smallest singular values with the full gain a^steps, 1.5 % of the result for the coefficients in use.  G made
@@ -39,7 +39,7 @@
 // shares, 5 x 10.3 us passes, each a launch, its waits for its matrix's entry, for G and for X, and one chunk of most wavefronts.
 // Rank 128 at 8192 / 22016, 178 MB: 253 us, of 66, 5 x 5.1 and 4 x 32 + 49 us: X, 45 MB, goes through memory in every pass at
 // 2.8 TB/s, beside 170 matrix instructions and 600 others a chunk of one wavefront a SIMD (its sums and operands take more than half
-// of the registers).  Two adapters of 1024 at rank 16: 37 us, one launch, bound by the instructions of its two compute units.
+// of the registers).  Two adapters of 1024 at rank 16: 33 us, six launches of 5 us, most of each waits for memory one after the other (one launch: 38).
 // Tried: operands of P and X through LDS, 64 columns a block, with the searches and barriers of the time: 57, 107 and 266 us.
 #include <algorithm>
 #include <type_traits>
@@ -339,7 +339,10 @@ constexpr size_t muon_p_lds(int rt) { return (size_t)rt * rt * 4096; }
 constexpr size_t muon_turn_lds(int rt) { return muon_waves(rt) * muon_turn_floats(rt) * 4; }
 constexpr size_t muon_start_lds(int rt) { return std::max(muon_share_lds(rt), muon_turn_lds(rt)); }
 constexpr size_t muon_alone_lds(int rt) { return 2 * muon_p_lds(rt) + muon_start_lds(rt); }
-constexpr size_t muon_pass_lds(int rt, bool last) { return last ? muon_p_lds(rt) + muon_turn_lds(rt) : std::max(muon_share_lds(rt), muon_p_lds(rt)); }
+constexpr size_t muon_pass_lds(int rt, bool last, bool direct) {  // (the shares lie where P and G have been)
+  const size_t p = muon_p_lds(rt) * (direct ? 2 : 1);
+  return last ? p + muon_turn_lds(rt) : std::max(muon_share_lds(rt), p);
+}
 
 // G's tiles from 32 columns of X as operands, rows of X as rows: g[(a, b)] += x_a x_b^T.
 template <int RT>
@@ -663,22 +666,45 @@ __global__ __launch_bounds__(256) void muon_reduce_kernel(const MuonTable table,
   put_gram<RT>(ws + t.gram, a, b, (at >> 6) & 3, at & 63, v);
 }
 
-// One step of the iteration.  first: X holds u, whose norm comes off here.
-template <int RT, bool LAST>
-__global__ __launch_bounds__(64 * muon_waves(RT), 1) void muon_pass_kernel(const MuonTable table, const MuonHyper h, bool first, float* ws) {
+// One step of the iteration (in the first one X holds u, whose norm comes off).  DIRECT: each block adds its matrix's shares of G by
+// itself, and leaves its share of the next one in the other of two places.
+template <int RT, bool LAST, bool DIRECT>
+__global__ __launch_bounds__(64 * muon_waves(RT), 1) void muon_pass_kernel(const MuonTable table, const MuonHyper h, int step, float* ws) {
   extern __shared__ __align__(16) f32x4 lds[];
   __shared__ float squares[muon_waves(RT)];
   int slice;
   const MuonTensor t = muon_find(table, table.block0, slice);
   const Columns<RT> w(t, ws, slice * table.per_block, min(t.chunks, (slice + 1) * table.per_block),
-                      reinterpret_cast<float*>(lds) + muon_p_lds(RT) / 4);
+                      reinterpret_cast<float*>(lds) + muon_p_lds(RT) / 4 * (DIRECT ? 2 : 1));
+  f32x4* partial = reinterpret_cast<f32x4*>(ws + t.partial);
+  const float* gram = ws + t.gram;
+  if constexpr (DIRECT) {
+    constexpr int NW = muon_waves(RT), PIECES = muon_upper(RT) * 4;  // of 64 times 16 bytes
+    const int slices = (t.chunks + table.per_block - 1) / table.per_block;
+    const size_t place = (size_t)slices * PIECES * 64;
+    const f32x4* src = partial + (step & 1 ? place : 0) + w.lane;
+    if (!(step & 1)) partial += place;
+    float* sum = reinterpret_cast<float*>(lds) + muon_p_lds(RT) / 4;
+#pragma unroll
+    for (int k = 0; k < (PIECES + NW - 1) / NW; ++k) {
+      const int piece = w.wave + NW * k;
+      if (piece >= PIECES) break;
+      f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
+      for (int z = 0; z < slices; ++z) v += src[((size_t)z * PIECES + piece) * 64];
+      int a, b;
+      upper_tile(piece >> 2, a, b);
+      put_gram<RT>(sum, a, b, piece & 3, w.lane, v);
+    }
+    lds_barrier();
+    gram = sum;
+  }
   // The columns that come next are on their way: the first ones while P is made, later ones while those before are worked on.
   f32x4 coming[4 * RT];
-  const Scales s = make_p<RT>(ws + t.gram, h, first, lds, squares, w.wave, w.lane, [&] { w.request(w.first, coming); });
+  const Scales s = make_p<RT>(gram, h, step == 0, lds, squares, w.wave, w.lane, [&] { w.request(w.first, coming); });
   f32x16 g[muon_upper(RT)];
   pass_columns<RT, LAST>(w, h, s, lds, coming, g);
-  if constexpr (!LAST)
-    store_share<RT>(g, lds, reinterpret_cast<f32x4*>(ws + t.partial) + (size_t)slice * muon_upper(RT) * 256, w.wave, w.lane);
+  if constexpr (!LAST) store_share<RT>(g, lds, partial + (size_t)slice * muon_upper(RT) * 256, w.wave, w.lane);
 }
 
 // All steps of a matrix in one block, G in its LDS: the launches above take 5 to 7 us each however little there is to do.
@@ -721,15 +747,17 @@ hipError_t launch(Kernel kern, int blocks, int rt, size_t lds, std::atomic<uint6
   return hipGetLastError();
 }
 
-template <int RT>
+template <int RT, bool DIRECT>
 hipError_t launch_steps(const MuonTable& t, const MuonHyper& h, int steps, float* ws, hipStream_t st) {
   static std::atomic<uint64_t> granted[3];
   if (hipError_t e = launch(muon_start_kernel<RT>, t.blocks, RT, muon_start_lds(RT), granted[0], st, t, h, ws); e != hipSuccess) return e;
   for (int k = 0; k < steps; ++k) {
-    muon_reduce_kernel<RT><<<t.reduce_blocks, 256, 0, st>>>(t, ws);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    const hipError_t e = k + 1 < steps ? launch(muon_pass_kernel<RT, false>, t.blocks, RT, muon_pass_lds(RT, false), granted[1], st, t, h, k == 0, ws)
-                                       : launch(muon_pass_kernel<RT, true>, t.blocks, RT, muon_pass_lds(RT, true), granted[2], st, t, h, k == 0, ws);
+    if constexpr (!DIRECT) {
+      muon_reduce_kernel<RT><<<t.reduce_blocks, 256, 0, st>>>(t, ws);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    const hipError_t e = k + 1 < steps ? launch(muon_pass_kernel<RT, false, DIRECT>, t.blocks, RT, muon_pass_lds(RT, false, DIRECT), granted[1], st, t, h, k, ws)
+                                       : launch(muon_pass_kernel<RT, true, DIRECT>, t.blocks, RT, muon_pass_lds(RT, true, DIRECT), granted[2], st, t, h, k, ws);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -745,8 +773,9 @@ hipError_t launch_alone(const MuonTable& t, const MuonHyper& h, int steps, float
 
 hipError_t launch_muon(const MuonTable& t, const MuonHyper& h, int steps, float* ws, hipStream_t st) {
   if (t.alone) return t.tiles == 2 ? launch_alone<2>(t, h, steps, ws, st) : launch_alone<1>(t, h, steps, ws, st);
-  if (t.tiles > 2) return launch_steps<4>(t, h, steps, ws, st);
-  return t.tiles == 2 ? launch_steps<2>(t, h, steps, ws, st) : launch_steps<1>(t, h, steps, ws, st);
+  if (t.tiles > 2) return launch_steps<4, false>(t, h, steps, ws, st);
+  if (t.direct) return t.tiles == 2 ? launch_steps<2, true>(t, h, steps, ws, st) : launch_steps<1, true>(t, h, steps, ws, st);
+  return t.tiles == 2 ? launch_steps<2, false>(t, h, steps, ws, st) : launch_steps<1, false>(t, h, steps, ws, st);
 }
 
 }  // namespace qalora

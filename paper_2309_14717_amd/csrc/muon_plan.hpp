@@ -18,12 +18,13 @@ struct MuonTensor {
   float step_size;       // lr times the shape's scale
   size_t x;              // floats from the workspace's start: X as [chunks][tiles] of 32 x MUON_CHUNK
   size_t gram;           // the Gram matrix: [tiles][tiles] of 32 x 32
-  size_t partial;        // each block's share of it: the upper tiles
+  size_t partial;        // each block's share of it: the upper tiles (in two places where `direct`)
 };
 struct MuonTable {
   int n, blocks, reduce_blocks, per_block;
   int tiles;                      // 32-row tiles that every X has: 1, 2 or 4, rows beyond a shorter side being zero
   bool alone;                     // a block does all steps of a matrix
+  bool direct;                    // blocks add their matrix's shares of G by themselves
   int block0[MUON_MAX_TENSORS];   // first block of the launches over X; blocks of `per_block` chunks
   int reduce0[MUON_MAX_TENSORS];  // first block of the launch that adds the blocks' Gram matrices
   MuonTensor t[MUON_MAX_TENSORS];
@@ -35,9 +36,12 @@ constexpr int muon_upper_tiles(int tiles) { return tiles * (tiles + 1) / 2; }
 // makes P from the Gram matrix, and leaves a share of the next: more of them only repeat that).
 constexpr int muon_waves_of(int tiles) { return tiles > 2 ? 4 : 8; }
 constexpr int MUON_BLOCKS = 256;
-// One launch, a block for each matrix, where the longest has this many 32 x 32 tiles of X at most.  Two matrices, 5 steps, us (one
-// launch against eleven): 32 x 512 25 / 41, 1024 38 / 42, 1280 45 / 43; 64 x 512 48 / 56, 768 62 / 56; fourteen alike.
-constexpr int MUON_ALONE_TILES = 32;
+// One launch, a block for each matrix, where the longest has this many 32 x 32 tiles of X at most; and no launches that add the
+// blocks' shares of G, but every block for itself, where that is this many tiles at most.  Two matrices, 5 steps, us, with one launch, six
+// and eleven: 32 x 512 25 / 30 / 42, 768 32 / 32 / 42, 1024 38 / 34 / 42, 4096 - / 34 / 45, 11008 - / 46 / 53, 16384 - / 51 / 49;
+// 64 x 384 39 / 46 / 56, 640 53 / 50 / 56, 4096 - / 59 / 60, 8192 - / 75 / 65.  Fourteen likewise.
+constexpr int MUON_ALONE_TILES = 24;
+constexpr int MUON_DIRECT_TILES = 48;
 
 // Fills in the table from rows[] and cols[]; returns the workspace's floats, 0 where the list is not acceptable
 // (`unsupported` says whether a matrix has both sides above MUON_MAX_SHORT, rather than a bad argument).
@@ -65,6 +69,7 @@ inline size_t muon_table(int n, const int32_t* rows, const int32_t* cols, MuonTa
   table.alone = table.tiles <= 2 && most_chunks <= MUON_ALONE_TILES / table.tiles;
   const int waves = muon_waves_of(table.tiles), upper = muon_upper_tiles(table.tiles);
   table.per_block = (int)((chunks + MUON_BLOCKS * waves - 1) / (MUON_BLOCKS * waves)) * waves;
+  table.direct = table.tiles <= 2 && (most_chunks + table.per_block - 1) / table.per_block * upper <= MUON_DIRECT_TILES;
   size_t floats = 0;
   table.blocks = table.reduce_blocks = 0;
   for (int i = 0; i < n; ++i) {
@@ -79,7 +84,7 @@ inline size_t muon_table(int n, const int32_t* rows, const int32_t* cols, MuonTa
     t.gram = floats;
     floats += (size_t)table.tiles * table.tiles * 1024;
     t.partial = floats;
-    floats += (size_t)blocks * upper * 1024;
+    floats += (size_t)blocks * upper * 1024 * (table.direct ? 2 : 1);
   }
   for (int i = n; i < MUON_MAX_TENSORS; ++i) table.block0[i] = table.reduce0[i] = INT32_MAX;
   return floats;

@@ -53,7 +53,13 @@ LISTS = {
     "layer": [s for i, o in [(512, 512)] * 4 + [(512, 1408)] * 2 + [(1408, 512)] for s in ((i // 32, 64), (64, o))],
     "many": [(8 + k, 40 * k + 1) for k in range(32)],
     "long": [(64, 22016), (48, 20001)],
-    # at the longest sides that one launch takes, and one beyond
+    # at the longest sides that one launch takes, that one launch a pass takes, and one beyond
+    "one32": [(32, 768), (768, 31), (1, 1)],
+    "one64": [(64, 384), (384, 33), (50, 383), (64, 1)],
+    "each32": [(32, 769), (12288, 32), (9, 40), (31, 12287)],
+    "each64": [(64, 385), (4096, 64), (33, 4095), (1, 1)],
+    "sums32": [(32, 12289), (9, 40)],
+    "sums64": [(4097, 64), (7, 9)],
     "alone32": [(32, 1024), (1024, 32), (31, 1023), (1, 1), (9, 40)],
     "alone64": [(64, 512), (512, 33), (50, 511), (64, 1)],
     "beyond32": [(1025, 32), (9, 40), (1, 1)],
@@ -65,6 +71,8 @@ KINDS = {  # of launches: by the largest matrix
     "beyond32": (20, 1100),
     "beyond64": (44, 700),
     "beyond128": (80, 90),
+    "sums32": (8, 12300),
+    "sums64": (36, 4100),
 }
 
 
@@ -154,7 +162,7 @@ def test_several_steps_and_reruns(gpu_api):
     assert all(torch.equal(a, b) for a, b in zip(*runs))
 
 
-@pytest.mark.parametrize("long", [1000, 3000])  # one launch, and several
+@pytest.mark.parametrize("long", [600, 1000, 3000, 13000])  # one launch, one a pass, and two
 def test_zero_infinite_and_tiny_gradients(gpu_api, long):
     """A zero matrix moves nothing (a fresh adapter's A has the gradient zero); a NaN stays in its own matrix; gradients far
     below eps do not blow up."""
@@ -176,7 +184,7 @@ def test_zero_infinite_and_tiny_gradients(gpu_api, long):
     assert np.sqrt(((1 - p[3].astype(np.float64) - X) ** 2).sum()) <= bound + 2.0 ** -24 * np.sqrt(p[3].size)
 
 
-@pytest.mark.parametrize("name", ["mixed", "alone64"])
+@pytest.mark.parametrize("name", ["mixed", "alone64", "one64", "each32", "sums32"])
 def test_workspace_contents_do_not_matter(gpu_api, name):
     rng = np.random.default_rng(12)
     shapes = LISTS[name]
@@ -193,11 +201,11 @@ def test_workspace_contents_do_not_matter(gpu_api, name):
     assert e.value.status == gpu_api.EWORKSPACE
 
 
-@pytest.mark.parametrize("long", [1000, 3000])
+@pytest.mark.parametrize("long", [600, 1000, 3000, 13000])
 def test_captured_step_replays(gpu_api, long):
     """A captured step replayed with eager steps of other matrices between: state moves as by eager steps."""
     rng = np.random.default_rng(13)
-    shapes = [(32, 64), (64, 512) if long > 1000 else (24, 512), (16, long)]
+    shapes = [(32, 64), (64, 512) if long == 3000 else (24, 512), (16, long)]
     g = up([gradient(rng, *s) for s in shapes])
     p0, z = [rng.standard_normal(s).astype(np.float32) for s in shapes], [np.zeros(s, np.float32) for s in shapes]
     hp = gpu_api.Muon(lr=0.05)

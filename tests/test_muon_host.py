@@ -18,7 +18,7 @@ extern "C" long long plan(int n, const int* rows, const int* cols, int* unsuppor
   return (long long)floats;
 }
 extern "C" void totals(long long* out) {
-  out[0] = table.blocks; out[1] = table.reduce_blocks; out[2] = table.per_block; out[3] = table.tiles; out[4] = table.alone;
+  out[0] = table.blocks; out[1] = table.reduce_blocks; out[2] = table.per_block; out[3] = table.tiles; out[4] = table.alone; out[5] = table.direct;
 }
 extern "C" void tensor(int i, long long* out) {
   const MuonTensor& t = table.t[i];
@@ -38,7 +38,7 @@ def plan(tmp_path_factory):
         arr = ctypes.c_int * max(n, 1)
         u = ctypes.c_int()
         floats = lib.plan(n, arr(*(r for r, _ in shapes)), arr(*(c for _, c in shapes)), ctypes.byref(u))
-        tot, ts = (ctypes.c_longlong * 5)(), []
+        tot, ts = (ctypes.c_longlong * 6)(), []
         lib.totals(tot)
         for i in range(n if floats else 0):
             t = (ctypes.c_longlong * 7)()
@@ -56,7 +56,7 @@ def test_table_covers_every_matrix_once(plan):
     lists += [[(1, 1)], [(128, 2 ** 27)], [(2 ** 27, 1)], [(128, 128)] * 32, [(64, 1000000)] * 32]
     for shapes in lists:
         shapes = [s if rng.random() < 0.5 else s[::-1] for s in shapes]
-        floats, unsupported, (blocks, reduce_blocks, per_block, tiles, alone), ts = plan(shapes)
+        floats, unsupported, (blocks, reduce_blocks, per_block, tiles, alone, direct), ts = plan(shapes)
         assert floats > 0 and not unsupported
         end = block = reduce = 0
         for (rows, cols), (_, chunks, block0, reduce0, x, gram, partial) in zip(shapes, ts):
@@ -65,9 +65,10 @@ def test_table_covers_every_matrix_once(plan):
             slices, upper = -(-chunks // per_block), tiles * (tiles + 1) // 2
             assert (block0, reduce0, x) == (block, reduce, end)           # regions follow each other without a gap
             assert gram == x + chunks * tiles * 32 * 32 and partial == gram + tiles * tiles * 1024
-            end, block, reduce = partial + slices * upper * 1024, block + slices, reduce + 8 * upper
+            end, block, reduce = partial + slices * upper * 1024 * (1 + direct), block + slices, reduce + 8 * upper
             assert x % 4 == gram % 4 == partial % 4 == 0                  # 16-byte accesses
-        assert alone == (tiles < 4 and max(max(s) for s in shapes) <= 1024 // tiles)
+        assert direct == (tiles < 4 and -(-max(t[1] for t in ts) // per_block) * tiles * (tiles + 1) // 2 <= 48)
+        assert alone == (tiles < 4 and max(max(s) for s in shapes) <= 768 // tiles)
         assert max(min(s) for s in shapes) > (32 * tiles // 2 if tiles > 1 else 0)
         assert (floats, blocks, reduce_blocks) == (end, block, reduce) and blocks < 2 ** 31
 
