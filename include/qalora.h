@@ -270,7 +270,8 @@ int qalora_forward_deployed_epilogue(const qalora_desc* desc, int tokens, const 
  * dz is the dy of qalora_backward.  All [tokens, cols], cols a multiple of 8 up to 2^29 (QALORA_EUNSUPPORTED otherwise); arithmetic in
  * fp32, dz and dmul rounded to bf16, dbias the sum of the unrounded values.
  * in : dy fp32 or bf16 per dy_dtype; z bf16, NULL allowed where neither act nor dmul needs it; mul bf16 or NULL
- * out: dz, dmul bf16, dbias fp32 [cols]: at least one, the others NULL; dmul only with mul; a bf16 dz may be dy itself.
+ * out: dz, dmul bf16, dbias fp32 [cols]: at least one, the others NULL; dmul only with mul.  dz or dmul may be z, mul or, where dy is
+ *      bf16, dy itself; any other overlap of an output with an input or another output is refused (QALORA_EINVAL).
  *      accumulate = 1 adds to dbias.  The slope of relu at zero is zero.
  * ws: qalora_epilogue_backward_workspace_bytes(tokens, cols) bytes, needed for dbias (0: none is).  Reruns are bit-identical; may be
  * captured into a HIP graph. */

@@ -18,6 +18,21 @@ constexpr size_t kAlign = 256;
 inline size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
+// A run of memory; null: none.
+struct Span {
+  const void* at;
+  size_t bytes;
+};
+inline bool overlap(const Span& a, const Span& b) {
+  const uintptr_t p = reinterpret_cast<uintptr_t>(a.at), q = reinterpret_cast<uintptr_t>(b.at);
+  return p && q && p < q + b.bytes && q < p + a.bytes;
+}
+// Whether writing `out` spoils `in`.  Where both hold elements of one size from one start on, the thread that writes an element is the one
+// that has read it: no harm.  Otherwise elements lie over others that other blocks have yet to read.
+inline bool spoils(const Span& out, const Span& in) {
+  return overlap(out, in) && !(out.at == in.at && out.bytes == in.bytes);
+}
+
 int row_align_for_bits(int bits) { return bits == 4 ? 8 : (bits == 2 ? 16 : 32); }
 
 // Workspace plans.  Offsets are a pure function of (desc, tokens), so the size query and
@@ -690,6 +705,12 @@ int qalora_epilogue_backward(int act, int tokens, int cols, const void* dy, int 
   if (cols % 8 != 0 || cols > EB_MAX_COLS) return QALORA_EUNSUPPORTED;
   const size_t need = dbias ? epilogue_back_floats(tokens, cols) * sizeof(float) : 0;
   if (need > 0 && (!ws || ws_bytes < need)) return QALORA_EWORKSPACE;
+  const size_t n = (size_t)tokens * cols;
+  const Span in[3] = {{dy, n * (dy_dtype == QALORA_BF16 ? 2 : 4)}, {z, 2 * n}, {mul, 2 * n}};
+  const Span o_dz{dz, 2 * n}, o_dmul{dmul, 2 * n}, o_dbias{dbias, sizeof(float) * cols};
+  if (overlap(o_dz, o_dmul) || overlap(o_dbias, o_dz) || overlap(o_dbias, o_dmul)) return QALORA_EINVAL;
+  for (const Span& i : in)
+    if (spoils(o_dz, i) || spoils(o_dmul, i) || overlap(o_dbias, i)) return QALORA_EINVAL;
   EpilogueBackArgs a{};
   a.dy = dy;
   a.z = static_cast<const uint16_t*>(z);
