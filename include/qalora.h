@@ -30,7 +30,7 @@
  *     8 bytes per token).  ws contents are undefined afterwards.  Two calls that may run
  *     at the same time (different streams) must not share a workspace.
  *   - Stream capture: forward, backward and merge -- and the _keep / _kept, _shared,
- *     _deployed and _noalloc forms -- may be captured into a HIP graph and
+ *     _deployed, _epilogue and _noalloc forms -- may be captured into a HIP graph and
  *     replayed (they enqueue kernels only: no memset, copy, allocation or event unless
  *     qalora_profile_arm armed one).  Make one eager call of the same shape first: the
  *     first use of a kernel sets its dynamic-LDS attribute, which is not stream work.  The
@@ -242,9 +242,11 @@ int qalora_backward_kept(const qalora_desc* desc, int tokens, const void* dy, co
  *   act       relu; silu(z) = z / (1 + exp(-z)); gelu(z) = z Phi(z); or its form by tanh,
  *             0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3)))
  *   bias      fp32 [d_out]
- *   mul       bf16 [tokens, d_out]: with the up projection here, the gate's call gives a SwiGLU block's hidden activations
+ *   mul       bf16 [tokens, d_out]: with the up projection here, the gate's call gives a SwiGLU block's hidden activations; it may
+ *             be a bf16 y itself
  *   residual  [tokens, d_out] of y's type; it may be y itself (the residual stream is then updated in place)
- *   z         out, bf16 [tokens, d_out]: z rounded, for qalora_epilogue_backward; not y, mul or residual
+ *   z         out, bf16 [tokens, d_out]: z rounded, for qalora_epilogue_backward
+ * Any other overlap of y, z or kept with each other or with x, bias, mul or residual is refused (QALORA_EINVAL).
  * qalora_forward_epilogue is qalora_forward with it, or, where kept is not NULL, qalora_forward_keep;
  * qalora_forward_deployed_epilogue is qalora_forward_deployed with it.  Same kernels, workspaces, precision of
  * the product (few tokens: exact operands), limits and status word: y is what the epilogue makes of the sums that these calls

@@ -554,6 +554,24 @@ static int forward_mid(const qalora_desc& d, int tokens, const void* x, const vo
   return launch_midt(d.bits, a, blocks, st) == hipSuccess ? 0 : 1;
 }
 
+// Whether an output of a forward with an epilogue lies over an operand that is still read, or over another output.
+static bool epilogue_overlaps(const qalora_desc& d, int tokens, const void* x, const Epilogue& e, const void* y, int y_dtype,
+                              const void* kept) {
+  const size_t n = (size_t)tokens * d.d_out, y_bytes = n * (y_dtype == QALORA_BF16 ? 2 : 4);
+  const Span out[3] = {{y, y_bytes}, {e.z, 2 * n}, {kept, kept ? qalora_kept_bytes(&d, tokens) : 0}};
+  const Span in[2] = {{x, 2 * (size_t)tokens * d.d_in}, {e.bias, sizeof(float) * d.d_out}};
+  const Span at_y[2] = {{e.mul, 2 * n}, {e.residual, y_bytes}};  // an element of these is read only for y's of the same place
+  for (int i = 0; i < 3; ++i) {
+    for (const Span& s : in)
+      if (overlap(out[i], s)) return true;
+    for (const Span& s : at_y)
+      if (i == 0 ? spoils(out[i], s) : overlap(out[i], s)) return true;
+    for (int k = 0; k < i; ++k)
+      if (overlap(out[i], out[k])) return true;
+  }
+  return false;
+}
+
 static int forward_impl(const qalora_desc* d, int tokens, const void* x, const void* packed,
                         const float* alpha, const float* beta, const PartSpec& ps, void* y, int y_dtype,
                         void* kept, bool keep, void* ws, size_t ws_bytes, void* stream,
@@ -579,6 +597,7 @@ static int forward_impl(const qalora_desc* d, int tokens, const void* x, const v
     // memory-bound regime: stream the weight once on the exact-operand path
     const size_t need = smallt_workspace(*d, tokens);
     if (!ws || ws_bytes < need) return QALORA_EWORKSPACE;
+    if (epi && epilogue_overlaps(*d, tokens, x, *epi, y, y_dtype, nullptr)) return QALORA_EINVAL;
     SmallTArgs a{};
     a.x = static_cast<const uint16_t*>(x);
     a.plane0 = static_cast<const uint32_t*>(packed);
@@ -600,6 +619,7 @@ static int forward_impl(const qalora_desc* d, int tokens, const void* x, const v
   }
   const FwdPlan plan = plan_forward(*d, tokens);
   if (!ws || ws_bytes < plan.total) return QALORA_EWORKSPACE;
+  if (epi && epilogue_overlaps(*d, tokens, x, *epi, y, y_dtype, keep ? kept : nullptr)) return QALORA_EINVAL;
   hipStream_t st = as_stream(stream);
   char* w = static_cast<char*>(ws);
   float2* rs = reinterpret_cast<float2*>(w + plan.rs);
@@ -989,6 +1009,7 @@ static int forward_deployed_impl(const qalora_desc* d, int tokens, const void* x
   }
   const size_t need = smallt_workspace(*d, tokens);
   if (!ws || ws_bytes < need) return QALORA_EWORKSPACE;
+  if (epi && epilogue_overlaps(*d, tokens, x, *epi, y, y_dtype, nullptr)) return QALORA_EINVAL;
   SmallTArgs a{};
   a.x = static_cast<const uint16_t*>(x);
   a.stream = deployed;

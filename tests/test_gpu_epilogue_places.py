@@ -2,6 +2,8 @@
 import pytest
 import torch
 
+import epilogue_cases as ec
+
 pytestmark = pytest.mark.gpu
 
 BF16, F32 = torch.bfloat16, torch.float32
@@ -26,3 +28,37 @@ def test_backward_in_the_place_of_its_operands(gpu_api, shape, dy_dtype):
         with pytest.raises(gpu_api.QaloraError) as e:
             gpu_api.epilogue_backward(dy, host[1].cuda(), "gelu", dz=over)
         assert e.value.status == gpu_api.EINVAL and torch.equal(dy.cpu(), host[0])
+
+
+@pytest.mark.parametrize("rank", [0, 24])
+@pytest.mark.parametrize("shape", [(1, 1024, 1024, 4, 32), (13, 512, 512, 2, 32), (20, 1024, 1024, 4, 32), (40, 4096, 2056, 4, 32),
+                                   (65, 1024, 264, 3, 32), (300, 512, 1032, 4, 32)], ids=str)
+def test_forward_in_the_place_of_mul_or_residual(gpu_api, shape, rank):
+    """y at a bf16 mul, at the residual, and at both at once, for each kernel that has an epilogue; refused over x and shifted."""
+    T, d_in, d_out, bits, group = shape
+    codes, alpha, beta, x, A, B = (None if t is None else t.cuda() for t in ec.drawn_layer(3, *shape, rank))
+    desc = gpu_api.make_desc(d_in, d_out, bits, group, rank, 0.25 if rank else 0.0)
+    packed = gpu_api.pack(desc, codes)
+    bias, mul, residual = (t.cuda() for t in ec.extras(4, T, d_out, BF16))
+
+    def call(mul, residual, **kw):
+        return gpu_api.forward_epilogue(desc, x, packed, alpha, beta, A, B, bias=bias, act="silu", mul=mul, residual=residual,
+                                        out_dtype=BF16, **kw)
+
+    ref, both = call(mul, residual), call(mul, mul)
+    place = mul.clone()
+    assert call(place, residual, y=place) is place and torch.equal(place, ref)
+    place = residual.clone()
+    assert call(mul, place, y=place) is place and torch.equal(place, ref)
+    place = mul.clone()
+    assert call(place, place, y=place) is place and torch.equal(place, both)
+    if d_in == d_out:
+        with pytest.raises(gpu_api.QaloraError) as e:
+            call(mul, x, y=x)
+        assert e.value.status == gpu_api.EINVAL
+    room = torch.zeros((T + 1, d_out), dtype=BF16, device="cuda")
+    for kw in (dict(mul=room[1:], residual=residual), dict(mul=mul, residual=room[1:])) if T > 1 else ():   # by a row
+        with pytest.raises(gpu_api.QaloraError) as e:
+            call(y=room[:-1], **kw)
+        assert e.value.status == gpu_api.EINVAL
+    assert not room.any()
