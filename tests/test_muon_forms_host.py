@@ -1,0 +1,29 @@
+"""The lists of muon_cases.py reach the forms of the orthogonalised update that they are named for (no GPU)."""
+import pytest
+
+from muon_cases import FORMS, chunks
+from test_muon_host import plan  # noqa: F401  (the launch table's host build)
+
+
+@pytest.mark.parametrize("name", sorted(FORMS))
+def test_lists_reach_their_forms(plan, name):  # noqa: F811
+    (tiles, alone, direct, in_a_row), shapes = FORMS[name]
+    floats, unsupported, (_, _, per_block, got_tiles, got_alone, got_direct), _ = plan(shapes)
+    assert floats > 0 and not unsupported
+    assert (got_tiles, bool(got_alone), bool(got_direct)) == (tiles, alone, direct)
+    waves = 8 if tiles < 4 else 4
+    if not alone:
+        assert per_block == waves * in_a_row
+        if in_a_row > 1:   # a wide and a tall matrix with full wavefronts, and blocks that end in between
+            assert max(chunks(s) for s in shapes if s[0] < s[1]) >= per_block
+            assert any(chunks(s) % per_block for s in shapes)
+    else:                  # wavefronts with several chunks, and with none
+        assert max(chunks(s) for s in shapes) > waves and min(chunks(s) for s in shapes) < waves
+
+
+def test_every_form_of_several_launches_has_a_list():
+    several = {form[:3] for form, _ in FORMS.values() if form[3] > 1}
+    assert several == {(1, False, True), (1, False, False), (2, False, True), (2, False, False), (4, False, False)}
+    for several_tall in ("direct1_two", "direct2_two", "sums2_two", "sums4_two", "sums4_three"):
+        form, shapes = FORMS[several_tall]
+        assert any(r > c and chunks((r, c)) > (8 if form[0] < 4 else 4) * form[3] for r, c in shapes)
