@@ -21,9 +21,11 @@ def test_lists_reach_their_forms(plan, name):  # noqa: F811
         assert max(chunks(s) for s in shapes) > waves and min(chunks(s) for s in shapes) < waves
 
 
-def test_every_form_of_several_launches_has_a_list():
-    several = {form[:3] for form, _ in FORMS.values() if form[3] > 1}
-    assert several == {(1, False, True), (1, False, False), (2, False, True), (2, False, False), (4, False, False)}
+def test_every_form_has_a_list():
+    seen = {form[:3] for form, _ in FORMS.values()}
+    assert seen == {(t, a, d) for t in (1, 2) for a, d in ((True, True), (False, True), (False, False))} | {(4, False, False)}
+    several = {form[:3] for form, _ in FORMS.values() if form[3] and form[3] > 1}
+    assert several == {form for form in seen if not form[1]}
     for several_tall in ("direct1_two", "direct2_two", "sums2_two", "sums4_two", "sums4_three"):
         form, shapes = FORMS[several_tall]
         assert any(r > c and chunks((r, c)) > (8 if form[0] < 4 else 4) * form[3] for r, c in shapes)
