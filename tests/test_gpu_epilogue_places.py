@@ -62,3 +62,27 @@ def test_forward_in_the_place_of_mul_or_residual(gpu_api, shape, rank):
             call(y=room[:-1], **kw)
         assert e.value.status == gpu_api.EINVAL
     assert not room.any()
+
+
+@pytest.mark.parametrize("shape", [(3, 1024, 520, 4, 32), (2, 1024, 520, 3, 32), (13, 512, 520, 2, 32), (20, 1024, 1032, 4, 32), (40, 4096, 2056, 4, 32),
+                                   (65, 1024, 264, 3, 32), (130, 512, 1032, 4, 32)], ids=str)
+def test_a_row_that_is_nan_stays_nan(gpu_api, shape):
+    """NaN sums, as a kernel leaves them where a wait ran out (no call can bring that about; here by a NaN in x), come through
+    every activation, a mul of zeros, a residual in place and z; the other rows are those of the same call without the NaN."""
+    T, d_in, d_out, bits, group = shape
+    codes, alpha, beta, x, _, _ = (None if t is None else t.cuda() for t in ec.drawn_layer(5, *shape))
+    desc = gpu_api.make_desc(d_in, d_out, bits, group)
+    packed = gpu_api.pack(desc, codes)
+    bias, mul, residual = (t.cuda() for t in ec.extras(6, T, d_out, BF16))
+    mul[:, ::2] = 0
+    at = T // 2
+    sick = x.clone()
+    sick[at, 5] = float("nan")
+    others = [t for t in range(T) if t != at]
+    for act in ec.ACTS:
+        def call(x):
+            stream = residual.clone()
+            return gpu_api.forward_epilogue(desc, x, packed, alpha, beta, bias=bias, act=act, mul=mul, residual=stream, keep_z=True,
+                                            out_dtype=BF16, y=stream)[:2]
+        for got, clean in zip(call(sick), call(x)):
+            assert torch.isnan(got[at]).all() and torch.equal(got[others], clean[others]), act
