@@ -429,9 +429,15 @@ int qalora_adamw_step(const qalora_adamw* hp, int step, int n_tensors, float* co
  * A matrix with an infinity or a NaN in u, or |u|_F above 1.8e19, becomes NaN, the others do not see it.  |u|_F below 2^-47 counts
  * as 2^-47 in X0.
  * ws: qalora_muon_workspace_bytes(n_tensors, rows, cols) bytes (0 for a list that is not acceptable): what the matrices take
- * themselves with every shorter side padded to 32, 64 or 128 (the same for all), and up to 14 MB.  fp32 arithmetic, sums in a fixed order: a step is bit-reproducible.  Errors of the sums, about 2^-24 of
- * |u|_F, grow with the smallest singular values, by up to a^steps.  May be captured into a HIP graph, after an eager call
- * with the same list and steps.  (Which matrices are in a list decides how its sums are split: a matrix's last bits may differ in another list.) */
+ * themselves with every shorter side padded to 32, 64 or 128 (the same for all) and every longer one to a multiple of 32, and up to
+ * 14 MB.
+ * Arithmetic: m, u, X, G and P are fp32, and so are all sums, in a fixed order: a step is bit-reproducible.  The operands of the matrix
+ * products (u, X, G, P) are held as two fp16 each, to 2^-23 of the value (or 2^-39 of its bound, |X|_F for an element of X, where
+ * that is more), and the product of their lower parts is left out: a product is off by up to 2^-21 of itself, 2^-23.7 in the root
+ * mean square, where fp32 operands would be exact.  Sums of n columns in a row, n the total of the longer sides / 2048 (/ 1024 with
+ * more than 64 rows) and at least 32, add about sqrt(n) / 2 times 2^-24.  These errors grow with the smallest singular values, by up
+ * to a^steps.  May be captured into a HIP graph, after an eager call with the same list and steps.  (Which matrices are in a list
+ * decides how its sums are split: a matrix's last bits may differ in another list.) */
 #define QALORA_MUON_MAX_TENSORS 32
 #define QALORA_MUON_MAX_SHORT 128
 #define QALORA_MUON_MAX_STEPS 16

@@ -20,9 +20,12 @@
 // anew from X in every pass keeps it at 2^-24 times the gain.)
 //
 // Products.  X, G and P are fp32; for the matrix cores a value v is split in two fp16, hi = fp16(S v) and lo = fp16(S v - hi), S a
-// power of two that keeps S v below 2^15.  Three products, hi hi + hi lo + lo hi, miss 2^-24 of the operands, as rounding them
-// to fp32 does, wherever S v is above 1/2 or so (below, lo is an fp16 subnormal: 2^-25 in all, however small S v), and take a fifth
-// of the time of the fp32 instruction (which has a sixteenth of the fp16 rate).  S comes from bounds: |G_ij| <= trace G,
+// power of two that keeps S v below 2^15.  hi has 11 bits and lo 11 with a sign, where v has 24: a value in four loses its last bit,
+// 2^-23 of it, while S v is above 1/4 (below, lo is an fp16 subnormal and 2^-25 / S is lost, however small v).  Three products,
+// hi hi + hi lo + lo hi, leave out lo lo, up to 2^-22: a product is off by 2^-21 of itself at worst and 2^-23.7 in the root mean square,
+// where fp32 operands are exact and only the sums round.  That is a choice for speed: three such products take a fifth of the time of
+// the fp32 instruction (which has a sixteenth of the fp16 rate), and five passes of the recipe with exact sums are off by 8e-7 of the result, with sums in
+// fp32 alone by 4e-7; a fourth product for lo lo would leave the root mean square at 2^-23.9.  S comes from bounds: |G_ij| <= trace G,
 // |X_ij| <= |X|_F = sqrt(trace G), |P_ij| <= |P|_F, and of P X their product; the values of most weight are then 2^3 and more,
 // P X's 2^-2.
 //

@@ -179,3 +179,26 @@ def test_norms_that_squares_lose(gpu_api, name, eps):
         e = 3 * (8 + np.sqrt(max(32 * row, 256)) / 2) * 2.0 ** -24
         assert np.linalg.norm(-dp[i].cpu().numpy().astype(np.float64) - A ** 5 * X0) <= A ** 5 * (
             2.0 ** -39 * X0.size ** 0.5 + 5 * e * np.linalg.norm(X0)), s
+
+
+@pytest.mark.parametrize("name", ["alone1", "alone2", "direct1", "direct2", "sums1", "sums2", "sums4", "sums4_two"])
+def test_a_product_by_itself(gpu_api, name):
+    """With b = c = 0 the one step is X = a X0, element by element one product of split operands: 2^-21 (8 half steps of fp32).  X0's
+    element, a's square in |P|_F (which only sets a scale: none), y's scale back (a power of two: none), the step size and the
+    parameter are rounded once each (3), and the norm, common to all elements, in its squares' products and sums (half of 8 + sqrt(n) / 2), its
+    root, eps, and reciprocal (3)."""
+    rng = np.random.default_rng(27)
+    shapes, row = form(name)
+    g = [(rng.uniform(0.5, 1, s) * rng.choice([-1, 1], s)).astype(np.float32) for s in shapes]
+    a = float(np.float32(1.7))
+    hp = gpu_api.Muon(lr=1.0, momentum=0.0, a=a, b=0.0, c=0.0, steps=1, nesterov=False, scale_mode=0)
+    dp = zeros(shapes)
+    gpu_api.muon_step(hp, dp, up(g), zeros(shapes))
+    worst = 0.0
+    for i, s in enumerate(shapes):
+        ref = -a * g[i].astype(np.float64) / (np.linalg.norm(g[i].astype(np.float64)) + float(hp.eps))
+        off = (np.abs(dp[i].cpu().numpy() - ref) / np.abs(ref)).max()
+        limit = (8 + 3 + 4 + np.sqrt(max(32 * row, 256)) / 4 + 3) * 2.0 ** -24
+        worst = max(worst, off / 2.0 ** -24)
+        assert off <= limit, s
+    record(f"muon product {name}", half_steps=worst)
