@@ -420,7 +420,10 @@ int qalora_adamw_step(const qalora_adamw* hp, int step, int n_tensors, float* co
  *   p = p (1 - lr weight_decay) - lr scale X.
  * (3.4445, -4.7750, 2.0315) with five steps are the published coefficients (K. Jordan, Muon, 2024): they bring singular
  * values from 2e-3 of |u|_F on to 0.7 .. 1.2; (1.5, -0.5, 0) converges to one, but slowly.
- * scale: 1; sqrt(max(1, rows / cols)); or 0.2 sqrt(max(rows, cols)), the mean square of an AdamW step.
+ * scale: 1; sqrt(max(1, rows / cols)); or 0.2 sqrt(max(rows, cols)), with which an element moves as far as in an AdamW step (0.2 lr
+ * in the root mean square).  The second is the published factor sqrt(max(1, out / in)) for weights stored [out, in].  A [L, r] and
+ * B [r, d_out] lie as [in, out], for which that factor is f = sqrt(max(1, cols / rows)), not this scale: where it is wanted, matrices
+ * of one f go into a list of their own with QALORA_MUON_SCALE_NONE, lr f and weight_decay / f.
  * params, grads, momentum: HOST arrays of n_tensors DEVICE pointers (fp32, row-major, 16-byte aligned, no two overlapping:
  * QALORA_EINVAL);
  * params and momentum are updated in place; grads are read, and set to zero afterwards if zero_grads != 0.
@@ -435,7 +438,7 @@ int qalora_adamw_step(const qalora_adamw* hp, int step, int n_tensors, float* co
  * products (u, X, G, P) are held as two fp16 each, to 2^-23 of the value (or 2^-39 of its bound, |X|_F for an element of X, where
  * that is more), and the product of their lower parts is left out: a product is off by up to 2^-21 of itself, 2^-23.7 in the root
  * mean square, where fp32 operands would be exact.  Sums of n columns in a row, n the total of the longer sides / 2048 (/ 1024 with
- * more than 64 rows) and at least 32, add about sqrt(n) / 2 times 2^-24.  These errors grow with the smallest singular values, by up
+ * more than 64 rows) and at least 96, add about sqrt(n) / 2 times 2^-24.  These errors grow with the smallest singular values, by up
  * to a^steps.  May be captured into a HIP graph, after an eager call with the same list and steps.  (Which matrices are in a list
  * decides how its sums are split: a matrix's last bits may differ in another list.) */
 #define QALORA_MUON_MAX_TENSORS 32

@@ -802,6 +802,8 @@ def adamw_step(hp: AdamW, step: int, params, grads, exp_avg, exp_avg_sq, zero_gr
     _check(rc, "qalora_adamw_step")
 
 
+# 1; sqrt(max(1, rows / cols)), the published factor of weights stored [out, in] (A and B are [in, out]: see qalora_muon_step);
+# 0.2 sqrt(max(rows, cols))
 MUON_SCALE_NONE, MUON_SCALE_SHAPE, MUON_SCALE_RMS = 0, 1, 2
 
 

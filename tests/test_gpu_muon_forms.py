@@ -202,3 +202,19 @@ def test_a_product_by_itself(gpu_api, name):
         worst = max(worst, off / 2.0 ** -24)
         assert off <= limit, s
     record(f"muon product {name}", half_steps=worst)
+
+
+@pytest.mark.parametrize("shape", [(64, 1408), (40, 64), (128, 64)], ids=str)
+def test_the_published_factor_of_matrices_stored_in_out(gpu_api, shape):
+    """f = sqrt(max(1, out / in)) by way of lr f and weight_decay / f: p = p (1 - lr wd) - lr f X."""
+    rng = np.random.default_rng(28)
+    lr, wd, f = 0.02, 0.1, max(1.0, shape[1] / shape[0]) ** 0.5
+    g, p = [gradient(rng, *shape)], [rng.standard_normal(shape).astype(np.float32)]
+    hp = gpu_api.Muon(lr=lr * f, momentum=0.0, weight_decay=wd / f, scale_mode=gpu_api.MUON_SCALE_NONE, nesterov=False)
+    dp = up(p)
+    gpu_api.muon_step(hp, dp, up(g), zeros([shape]))
+    X, bound = recipe(g[0].astype(np.float64), 5, float(hp.eps), 1)
+    ref = p[0] * (1 - lr * wd) - lr * f * X
+    # lr f, weight_decay / f, the decay, the step size and the result are rounded once each
+    tol = 2.0 ** -24 * (4 * np.linalg.norm(p[0]) + 2 * lr * f * np.linalg.norm(X) + np.linalg.norm(ref))
+    assert distance(dp[0], ref) <= lr * f * bound + tol
