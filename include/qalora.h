@@ -240,7 +240,9 @@ int qalora_backward_kept(const qalora_desc* desc, int tokens, const void* dy, co
  *   z = x W~ + s (pool_g(x) A) B + bias;    y = act(z) * mul + residual.
  * Each member may be absent (NULL; QALORA_ACT_NONE); an epilogue without any, or NULL, is the plain linear.
  *   act       relu; silu(z) = z / (1 + exp(-z)); gelu(z) = z Phi(z); or its form by tanh,
- *             0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3)))
+ *             0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))).  Exponentials and reciprocals are the hardware's: act(z) is off by
+ *             up to (8 + 4 e) 2^-24 of itself, e the magnitude of the exponent: |z| for silu, z^2 for gelu, 2 sqrt(2/pi) |z + 0.044715 z^3|
+ *             for its form by tanh.  (An fp32 y shows that for negative z, where act(z) is small; below 1e-30 it may be zero.)
  *   bias      fp32 [d_out]
  *   mul       bf16 [tokens, d_out]: with the up projection here, the gate's call gives a SwiGLU block's hidden activations; it may
  *             be a bf16 y itself

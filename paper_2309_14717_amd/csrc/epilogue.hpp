@@ -19,7 +19,9 @@ struct Epilogue {
   int on;                // whether there is anything to do
 };
 
-// 1 / (1 + exp(-v)); zero and one where that is what fp32 holds
+// 1 / (1 + exp(-v)); zero and one where that is what fp32 holds.  The hardware's exponential takes v log2(e) rounded to fp32, so the
+// relative error grows by |v| 2^-24 (measured: 1.2 |v| + 2 half steps of fp32 at v = -85); for bf16 results, and for fp32 ones that a
+// sum follows, that is less than what follows.  erfc below grows by v^2 2^-24 likewise (1.3 v^2 measured).
 __device__ __forceinline__ float logistic(float v) { return __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
 constexpr float kTanhSlope = 1.5957691216057308f;  // 2 sqrt(2 / pi): 0.5 (1 + tanh(u)) = logistic(2 u)
 __device__ __forceinline__ float gelu_tanh_arg(float v) { return kTanhSlope * v * __builtin_fmaf(0.044715f * v, v, 1.0f); }

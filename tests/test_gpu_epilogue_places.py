@@ -86,3 +86,17 @@ def test_a_row_that_is_nan_stays_nan(gpu_api, shape):
                                             out_dtype=BF16, y=stream)[:2]
         for got, clean in zip(call(sick), call(x)):
             assert torch.isnan(got[at]).all() and torch.equal(got[others], clean[others]), act
+
+
+@pytest.mark.parametrize("act", ec.ACTS)
+def test_activations_in_fp32(gpu_api, act):
+    """act(z) in an fp32 y to the documented (8 + 4 e) 2^-24 of itself: v log2(e) rounded and its constant (2 half steps of e and 1 of the
+    exponent's conversion, below 4 e in all), the exponential, the sum, the reciprocal and the products (2 + 1 + 2 + 2, below 8)."""
+    n, g = 1 << 16, torch.Generator().manual_seed(9)
+    packed = gpu_api.pack(gpu_api.make_desc(64, n, 4, 32), torch.zeros((64, n), dtype=torch.uint8, device="cuda"))
+    zero, x = torch.zeros((2, n), device="cuda"), torch.zeros((1, 64), dtype=BF16, device="cuda")
+    for low, high in ((-70, -30), (-30, -8), (-8, -1), (-1, 1), (1, 8), (8, 70)):
+        z = low + (high - low) * torch.rand(n, generator=g)
+        y = gpu_api.forward_epilogue(gpu_api.make_desc(64, n, 4, 32), x, packed, zero, zero, bias=z.cuda(), act=act)[0].cpu().double()
+        ref, _, e = ec.act64(z.double(), act)
+        assert ((y - ref).abs() <= (8 + 4 * e) * 2.0 ** -24 * ref.abs() + 1e-30).all(), (low, high)
