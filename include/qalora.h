@@ -434,8 +434,8 @@ int qalora_adamw_step(const qalora_adamw* hp, int step, int n_tensors, float* co
  * A matrix with an infinity or a NaN in u, or |u|_F above 1.8e19, becomes NaN, the others do not see it.  |u|_F below 2^-47 counts
  * as 2^-47 in X0.
  * ws: qalora_muon_workspace_bytes(n_tensors, rows, cols) bytes (0 for a list that is not acceptable): what the matrices take
- * themselves with every shorter side padded to 32, 64 or 128 (the same for all) and every longer one to a multiple of 32, and up to
- * 14 MB.
+ * themselves with every shorter side padded to 32, 64 or 128 (the same for all, so that few matrices of a far larger rank are better
+ * called by themselves) and every longer one to a multiple of 32, and up to 14 MB.
  * Arithmetic: m, u, X, G and P are fp32, and so are all sums, in a fixed order: a step is bit-reproducible.  The operands of the matrix
  * products (u, X, G, P) are held as two fp16 each, to 2^-23 of the value (or 2^-39 of its bound, |X|_F for an element of X, where
  * that is more), and the product of their lower parts is left out: a product is off by up to 2^-21 of itself, 2^-23.7 in the root

@@ -40,6 +40,12 @@ constexpr int MUON_BLOCKS = 256;
 // blocks' shares of G, but every block for itself, where that is this many tiles at most.  Two matrices, 5 steps, us, with one launch, six
 // and eleven: 32 x 512 25 / 30 / 42, 768 32 / 32 / 42, 1024 38 / 34 / 42, 4096 - / 34 / 45, 11008 - / 46 / 53, 16384 - / 51 / 49;
 // 64 x 384 39 / 46 / 56, 640 53 / 50 / 56, 4096 - / 59 / 60, 8192 - / 75 / 65.  Fourteen likewise.
+// Neither beyond 64 rows: G and P take 64 KB each there, and with the 68 KB that the last pass keeps for tall matrices, or the 80 KB of a
+// block's shares, more than the 160 KB of a compute unit (so two of 65 x 1024 take 99 us where two of 64 x 1024 take 53).
+// Both hold for the list, by its longest matrix, as do the tiles by its largest shorter side: a launch is one kernel for all matrices, and one
+// that a single matrix needs is made anyhow.  13 of 32 x 4096 and one of 32 x 22016: 58 in one list, 42 + 50 in two; 13 of 64 x 1024 and
+// one of 64 x 11008 72, 57 + 66.  Padding to the largest shorter side can cost that much: 14 of rank 16 and one of 128 x 4096 take 168, 48 + 103
+// in two lists.
 constexpr int MUON_ALONE_TILES = 24;
 constexpr int MUON_DIRECT_TILES = 48;
 
