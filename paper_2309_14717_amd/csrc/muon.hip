@@ -37,12 +37,13 @@
 // matrix cores, and goes back into them as it is; P, symmetric, likewise; and for X X^T, whose contraction runs over the columns,
 // the tile is turned by a product with the unit matrix, exact for hi and lo each.
 //
-// Measured, five passes: the seven adapters of a 4096 / 11008 layer at rank 64, 44 MB of p, g, m and X: 82 us (fp32 products of the
-// recipe alone 18 us at the card's rate, the bytes that cannot be spared 11 us): 15 us of momentum and first G, 5 x 4.2 us adding
-// shares, 5 x 10.3 us passes, each a launch, its waits for its matrix's entry, for G and for X, and one chunk of most wavefronts.
-// Rank 128 at 8192 / 22016, 178 MB: 253 us, of 66, 5 x 5.1 and 4 x 32 + 49 us: X, 45 MB, goes through memory in every pass at
-// 2.8 TB/s, beside 170 matrix instructions and 600 others a chunk of one wavefront a SIMD (its sums and operands take more than half
-// of the registers).  Two adapters of 1024 at rank 16: 33 us, six launches of 5 us, most of each waits for memory one after the other (one launch: 38).
+// Measured, five passes: the seven adapters of a 4096 / 11008 layer at rank 64, 44 MB of p, g, m and X: 81 us (the bytes that cannot be
+// spared 11 us, three fp16 products for each of the recipe's 6): 15 us of momentum and first G, 5 x 4.2 us adding shares, 5 x 10.3 us
+// passes, each a launch, its waits for its matrix's entry, for G and for X, and one chunk of most wavefronts.
+// Rank 128 at 8192 / 22016, 178 MB: 255 us, of 64, 5 x 5.0 and 4 x 32 + 49 us: X, 45 MB, comes from behind the L2 in every pass and goes
+// back there (counters: 49 MB read and 54 written a pass, 3.3 TB/s; 2.8 in the last, 3.0 in the first launch), beside 170 matrix instructions and 600 others
+// a chunk of one wavefront a SIMD (its sums and operands take more than half of the registers).  Two adapters of 1024 at rank 16: 33 us, six
+// launches of 5 us, most of each waits for memory one after the other (one launch: 38).
 // Tried: operands of P and X through LDS, 64 columns a block, with the searches and barriers of the time: 57, 107 and 266 us.
 #include <algorithm>
 #include <type_traits>
