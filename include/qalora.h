@@ -440,7 +440,7 @@ int qalora_adamw_step(const qalora_adamw* hp, int step, int n_tensors, float* co
  * products (u, X, G, P) are held as two fp16 each, to 2^-23 of the value (or 2^-39 of its bound, |X|_F for an element of X, where
  * that is more), and the product of their lower parts is left out: a product is off by up to 2^-21 of itself, 2^-23.7 in the root
  * mean square, where fp32 operands would be exact.  Sums of n columns in a row, n the total of the longer sides / 2048 (/ 1024 with
- * more than 64 rows) and at least 96, add about sqrt(n) / 2 times 2^-24.  These errors grow with the smallest singular values, by up
+ * more than 64 rows) and at least 96, add about sqrt(n) / 2 times 2^-24 at random signs.  These errors grow with the smallest singular values, by up
  * to a^steps.  May be captured into a HIP graph, after an eager call with the same list and steps.  (Which matrices are in a list
  * decides how its sums are split: a matrix's last bits may differ in another list.) */
 #define QALORA_MUON_MAX_TENSORS 32

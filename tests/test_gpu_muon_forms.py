@@ -218,3 +218,44 @@ def test_the_published_factor_of_matrices_stored_in_out(gpu_api, shape):
     # lr f, weight_decay / f, the decay, the step size and the result are rounded once each
     tol = 2.0 ** -24 * (4 * np.linalg.norm(p[0]) + 2 * lr * f * np.linalg.norm(X) + np.linalg.norm(ref))
     assert distance(dp[0], ref) <= lr * f * bound + tol
+
+
+def test_two_calls_at_once(gpu_api):
+    """Steps on two streams, and a linear with its epilogue and the backward of that beside them: as one after the other."""
+    rng = np.random.default_rng(29)
+    names = ("sums4_two", "direct2_two")
+    hp = gpu_api.Muon(lr=0.05)
+    start = {n: ([rng.standard_normal(s).astype(np.float32) for s in FORMS[n][1]], [gradient(rng, *s) for s in FORMS[n][1]]) for n in names}
+    desc = gpu_api.make_desc(512, 1032, 4, 32, 16, 0.25)
+    gen = torch.Generator("cuda").manual_seed(6)
+    codes = torch.randint(0, 16, (512, 1032), generator=gen, device="cuda", dtype=torch.uint8)
+    draw = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
+    weights = (gpu_api.pack(desc, codes), 0.01 * draw(16, 1032), 0.01 * draw(16, 1032), draw(16, 16), draw(16, 1032))
+    x, mul = draw(700, 512).to(torch.bfloat16), draw(700, 1032).to(torch.bfloat16)
+
+    def block():
+        y, z, _ = gpu_api.forward_epilogue(desc, x, *weights, act="gelu", mul=mul, keep_z=True, out_dtype=torch.bfloat16)
+        return [y, z, *gpu_api.epilogue_backward(y, z, "gelu", mul=mul, want_dbias=True)]
+
+    def steps(n, state):
+        for _ in range(3):
+            gpu_api.muon_step(hp, state[0], state[1], state[2])
+
+    state = {n: (up(p), up(g), zeros(FORMS[n][1])) for n, (p, g) in start.items()}
+    for n in names:
+        steps(n, state[n])
+    alone = block()
+    torch.cuda.synchronize()
+    again = {n: (up(p), up(g), zeros(FORMS[n][1])) for n, (p, g) in start.items()}
+    torch.cuda.synchronize()
+    streams, beside = [torch.cuda.Stream() for _ in range(3)], []
+    for s, n in zip(streams, names):
+        with torch.cuda.stream(s):
+            steps(n, again[n])
+    with torch.cuda.stream(streams[2]):
+        for _ in range(3):
+            beside.append(block())
+    torch.cuda.synchronize()
+    for n in names:
+        assert all(torch.equal(a, b) for x, y in zip(state[n], again[n]) for a, b in zip(x, y))
+    assert all(torch.equal(a, b) for got in beside for a, b in zip(got, alone))
