@@ -376,7 +376,8 @@ def _epilogue(T, d_out, dev, y, bias, act, mul, residual, z):
 def forward_epilogue(desc: Desc, x, packed, alpha, beta, A=None, B=None, bias=None, act="none", mul=None,
                      residual=None, keep_z=False, keep=False, out_dtype=torch.float32, ws=None, y=None, z=None, kept=None):
     """forward() with y = act(x W~ + ... + bias) * mul + residual (see qalora_forward_epilogue).  ``act`` is one of
-    ACTIVATIONS; ``residual`` has y's type and may be the ``y`` that is passed.  Returns y; or (y, z, kept) with
+    ACTIVATIONS; ``residual`` has y's type and may be the ``y`` that is passed, as may a ``mul`` where y is bfloat16; other
+    outputs over operands are refused.  Returns y; or (y, z, kept) with
     ``keep_z`` (z in bf16, for epilogue_backward) or ``keep`` (the pooled activations, for backward_kept), None in the place
     of the one not asked for."""
     out = _fast().forward_epilogue(desc, x, packed, alpha, beta, A, B, bias, ACTIVATIONS.get(act), mul, residual, keep_z, keep,
@@ -409,7 +410,8 @@ def forward_epilogue(desc: Desc, x, packed, alpha, beta, A=None, B=None, bias=No
 def epilogue_backward(dy, z=None, act="none", mul=None, want_dz=True, want_dbias=False, dz=None, dmul=None, dbias=None,
                       accumulate=False, ws=None):
     """Backward of the epilogue at the kept z (see qalora_epilogue_backward): (dz, dmul, dbias), None in the place of what
-    is not there: dmul without ``mul``, dbias unless wanted or given.  dz is the dy of backward(); the gradient of the
+    is not there: dmul without ``mul``, dbias unless wanted or given.  ``dz`` or ``dmul`` may be z, mul or a bfloat16 dy; other
+    overlaps are refused.  dz is the dy of backward(); the gradient of the
     residual is dy itself."""
     out = _fast().epilogue_backward(dy, z, ACTIVATIONS.get(act), mul, want_dz, want_dbias, dz, dmul, dbias, accumulate, ws)
     if out is not None:

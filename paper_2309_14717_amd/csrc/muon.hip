@@ -17,7 +17,7 @@
 //
 // (G alone could carry the whole iteration: P is a polynomial in the first G.  But an error of 2^-24 in that G then meets
 // the smallest singular values with the full gain a^steps, 1.5 % of the result for the coefficients in use.  G made
-// anew from X in every pass keeps it at 2^-24 times the gain.)
+// anew from X in every pass keeps it at its own products' and sums' error times the gain.)
 //
 // Products.  X, G and P are fp32; for the matrix cores a value v is split in two fp16, hi = fp16(S v) and lo = fp16(S v - hi), S a
 // power of two that keeps S v below 2^15.  hi has 11 bits and lo 11 with a sign, where v has 24: a value in four loses its last bit,
