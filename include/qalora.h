@@ -30,7 +30,7 @@
  *     8 bytes per token).  ws contents are undefined afterwards.  Two calls that may run
  *     at the same time (different streams) must not share a workspace.
  *   - Stream capture: forward, backward and merge -- and the _keep / _kept, _shared,
- *     _deployed, _epilogue and _noalloc forms -- may be captured into a HIP graph and
+ *     _deployed, _epilogue, _int8 and _noalloc forms -- may be captured into a HIP graph and
  *     replayed (they enqueue kernels only: no memset, copy, allocation or event unless
  *     qalora_profile_arm armed one).  Make one eager call of the same shape first: the
  *     first use of a kernel sets its dynamic-LDS attribute, which is not stream work.  The
@@ -283,6 +283,72 @@ size_t qalora_epilogue_backward_workspace_bytes(int tokens, int cols);
 int qalora_epilogue_backward(int act, int tokens, int cols, const void* dy, int dy_dtype, const void* z,
                              const void* mul, void* dz, void* dmul, float* dbias, int accumulate, void* ws,
                              size_t ws_bytes, void* stream);
+
+/* A linear in 8-bit integers: a frozen weight (or a merged layer for prompts and serving) and its activations as whole numbers
+ * with a scale for each output channel and for each token, products summed exactly in 32 bits.
+ *   tokens    v = x (bf16), or v = x factor[i] rounded to fp32;  s[t] = fl32(max_i |v[t,i]| / 127);
+ *             q[t,i] = the whole number nearest to the quotient v / s (ties to even; of the exact quotient, not of a rounded one).
+ *             A row of zeros has s = 0 and codes 0.  A row with an infinity or a NaN in v has s = NaN and codes 0, and so become the
+ *             results of that token (no others).
+ *   weights   the same for each output channel j over the inputs:  W[i,j] ~ scale[j] codes[j,i].  Any codes in -127 .. 127 and any
+ *             scales may be given to the products.
+ *   forward   z[t,j] = (acc s[t]) scale[j] + bias[j], acc = sum_i q[t,i] codes[j,i];  y = act(z) * mul + residual, in fp32, rounded once
+ *             (the epilogue of qalora_forward_epilogue: members, aliasing and precision as there).
+ *   backward  dx[t,i] = acc s[t] + residual[t,i], acc = sum_j q[t,j] codes[j,i], with q and s of v = dy[t,j] scale[j]: the gradient of the
+ *             forward with the codes of x taken for x, and with dy's own rounding to 8 bits per token (at most s / 2 an element of v).
+ *             The weight is frozen; the bias's gradient is qalora_epilogue_backward's.
+ * codes int8 [d_out, d_in], scale fp32 [d_out]: one copy serves both directions.  d_in a multiple of 16, d_out a multiple of 8, both at
+ * most QALORA_INT8_MAX_SIDE (the sums then fit 32 bits); QALORA_EUNSUPPORTED otherwise.  No other limit on sizes: operands may pass 4 GB.
+ * All of these may be captured into a HIP graph after one eager call of the same shape; reruns are bit-identical. */
+#define QALORA_INT8_MAX_SIDE 131072
+/* W fp32 [d_in, d_out] (row-major, as everywhere) -> codes [d_out, d_in], scale [d_out]. */
+int qalora_quantize_int8(int d_in, int d_out, const float* W, int8_t* codes, float* scale, void* stream);
+/* The same of a quantized layer's W~ = alpha code + beta (one rounding to fp32 an element), merged or without an adapter; rank and s of
+ * desc are ignored.  On top of the layer's own error an element is off by up to scale[j] / 2. */
+int qalora_deploy_int8(const qalora_desc* desc, const void* packed, const float* alpha, const float* beta,
+                       int8_t* codes, float* scale, void* stream);
+/* x bf16 [tokens, cols] -> q [tokens, cols], s [tokens]; cols a multiple of 8, at most QALORA_INT8_MAX_SIDE.  For linears that share
+ * an input, and for activations that are kept as tokens.  factor: fp32 [cols], or NULL. */
+int qalora_quantize_tokens(int tokens, int cols, const void* x, const float* factor /* or NULL */, int8_t* q, float* s,
+                           void* stream);
+/* x: bf16 [tokens, d_in], brought to 8 bits within the call (in the workspace); or, with x_scale (fp32 [tokens]), its codes, int8
+ * [tokens, d_in].  z (in the epilogue) is kept in bf16.
+ * ws: qalora_int8_workspace_bytes(tokens, d_in, d_out, QALORA_OP_FORWARD or QALORA_OP_BACKWARD) bytes (0 for sizes or an op that are not
+ * acceptable); that size also serves any smaller number of tokens. */
+size_t qalora_int8_workspace_bytes(int tokens, int d_in, int d_out, int op);
+int qalora_forward_int8(int tokens, int d_in, int d_out, const void* x, const float* x_scale /* or NULL */,
+                        const int8_t* codes, const float* scale, const qalora_epilogue* epilogue /* host, or NULL */,
+                        void* y, int y_dtype, void* ws, size_t ws_bytes, void* stream);
+/* dy bf16 [tokens, d_out]; residual, or NULL: [tokens, d_in] of dx's type, may be dx itself (several linears' gradients are then added up
+ * in place); any other overlap of dx with an operand is refused (QALORA_EINVAL). */
+int qalora_backward_int8(int tokens, int d_in, int d_out, const void* dy, const int8_t* codes, const float* scale,
+                         const void* residual /* or NULL */, void* dx, int dx_dtype, void* ws, size_t ws_bytes,
+                         void* stream);
+
+/* Activations kept in 8 bits for the backward, about half of bf16's room.  Of [tokens, cols], 32 neighbouring columns of a row (the last
+ * group of a row may be shorter) share an exponent E, the biased exponent of their largest magnitude (at least 1), and an element is
+ * the whole multiple of 2^(E - 133) nearest to it (ties to even), at most 127 of them: off by at most half a step, that is 2^-7 of
+ * the group's largest magnitude.  What comes back is a bf16 number.  A group with an infinity or a NaN comes back as NaN.
+ * kept: qalora_kept8_bytes(tokens, cols) bytes (0: sizes that are not acceptable), contents private to the library.  cols a multiple of 8 up to
+ * 2^29.  Nothing may overlap.  May be captured into a HIP graph. */
+size_t qalora_kept8_bytes(int tokens, int cols);
+int qalora_keep8(int tokens, int cols, const void* x, void* kept, void* stream);         /* x bf16 */
+int qalora_restore8(int tokens, int cols, const void* kept, void* x, void* stream);      /* x bf16 */
+/* SwiGLU on gu = [gate | up], bf16 [tokens, 2 cols], as qalora_swiglu_forward_wide (h is that call's bit for bit), with what follows it in the
+ * same pass; each output may be NULL, but not all:
+ *   h     bf16 [tokens, cols]
+ *   q, s  its codes and scales, as qalora_quantize_tokens makes them of the bf16 h: the down projection's input (together; cols at most
+ *         QALORA_INT8_MAX_SIDE, QALORA_EUNSUPPORTED otherwise)
+ *   kept  gate and up for the backward: what qalora_keep8 makes of gu as [2 tokens, cols], qalora_kept8_bytes(2 tokens, cols) bytes
+ * and the backward from what was kept: dgu = [dgate | dup], qalora_swiglu_backward_wide's on what qalora_restore8 gives back.  tokens at most
+ * 2^30 - 1. */
+int qalora_swiglu_forward8(int tokens, int cols, const void* gu, void* h, int8_t* q, float* s, void* kept, void* stream);
+int qalora_swiglu_backward_kept8(int tokens, int cols, const void* dh, const void* kept, void* dgu, void* stream);
+/* qalora_epilogue_backward with z and mul as qalora_keep8 kept them (z8, mul8; NULL as there; one at least is given).  dz or dmul may be a bf16
+ * dy itself; any other overlap is refused.  Workspace: qalora_epilogue_backward_workspace_bytes(tokens, cols). */
+int qalora_epilogue_backward_kept8(int act, int tokens, int cols, const void* dy, int dy_dtype, const void* z8,
+                                   const void* mul8, void* dz, void* dmul, float* dbias, int accumulate, void* ws,
+                                   size_t ws_bytes, void* stream);
 
 /* Several adapted linears that share their input x (q/k/v of an attention block; gate/up of a
  * SwiGLU MLP), evaluated as ONE wide layer: one pass over x (row scales, conversion, pooling --

@@ -42,6 +42,10 @@ EXPORTS = (
     "qalora_muon_workspace_bytes", "qalora_muon_step",
     "qalora_forward_epilogue", "qalora_forward_deployed_epilogue",
     "qalora_epilogue_backward_workspace_bytes", "qalora_epilogue_backward",
+    "qalora_quantize_int8", "qalora_deploy_int8", "qalora_quantize_tokens", "qalora_int8_workspace_bytes",
+    "qalora_forward_int8", "qalora_backward_int8",
+    "qalora_kept8_bytes", "qalora_keep8", "qalora_restore8", "qalora_swiglu_forward8", "qalora_swiglu_backward_kept8",
+    "qalora_epilogue_backward_kept8",
 )
 
 
@@ -124,6 +128,20 @@ def load() -> ctypes.CDLL:
     lib.qalora_epilogue_backward_workspace_bytes.restype = sz
     lib.qalora_epilogue_backward_workspace_bytes.argtypes = [i, i]
     lib.qalora_epilogue_backward.argtypes = [i, i, i, vp, i, vp, vp, vp, vp, vp, i, vp, sz, vp]
+    lib.qalora_quantize_int8.argtypes = [i, i, vp, vp, vp, vp]
+    lib.qalora_deploy_int8.argtypes = [cp, vp, vp, vp, vp, vp, vp]
+    lib.qalora_quantize_tokens.argtypes = [i, i, vp, vp, vp, vp, vp]
+    lib.qalora_int8_workspace_bytes.restype = sz
+    lib.qalora_int8_workspace_bytes.argtypes = [i, i, i, i]
+    lib.qalora_forward_int8.argtypes = [i, i, i, vp, vp, vp, vp, vp, vp, i, vp, sz, vp]
+    lib.qalora_backward_int8.argtypes = [i, i, i, vp, vp, vp, vp, vp, i, vp, sz, vp]
+    lib.qalora_kept8_bytes.restype = sz
+    lib.qalora_kept8_bytes.argtypes = [i, i]
+    lib.qalora_keep8.argtypes = [i, i, vp, vp, vp]
+    lib.qalora_restore8.argtypes = [i, i, vp, vp, vp]
+    lib.qalora_swiglu_forward8.argtypes = [i, i, vp, vp, vp, vp, vp, vp]
+    lib.qalora_swiglu_backward_kept8.argtypes = [i, i, vp, vp, vp, vp]
+    lib.qalora_epilogue_backward_kept8.argtypes = [i, i, i, vp, i, vp, vp, vp, vp, vp, i, vp, sz, vp]
     lib.qalora_muon_workspace_bytes.restype = sz
     lib.qalora_muon_workspace_bytes.argtypes = [i, vp, vp]
     lib.qalora_muon_step.argtypes = [vp, i, vp, vp, vp, vp, vp, i, vp, sz, vp]
@@ -944,6 +962,242 @@ def swiglu_backward_strided(dh, gu, cols, out=None):
     _check(load().qalora_swiglu_backward_wide(_p(dh), _p(gu), _p(out), rows, cols, _stream()),
            "qalora_swiglu_backward_wide")
     return out
+
+
+def quantize_int8(W):
+    """W fp32 [d_in, d_out] -> (codes int8 [d_out, d_in], scale fp32 [d_out]): a frozen weight for forward_int8 and backward_int8."""
+    _need(W, "W", torch.float32)
+    if W.dim() != 2:
+        raise ValueError(f"W: shape {tuple(W.shape)}, expected [d_in, d_out]")
+    (d_in, d_out), dev = W.shape, W.device
+    codes = torch.empty((d_out, d_in), dtype=torch.int8, device=dev)
+    scale = torch.empty(d_out, dtype=torch.float32, device=dev)
+    with _on(dev):
+        rc = load().qalora_quantize_int8(d_in, d_out, _p(W), _p(codes), _p(scale), _stream())
+    _check(rc, "qalora_quantize_int8")
+    return codes, scale
+
+
+def deploy_int8(desc: Desc, packed, alpha, beta):
+    """The 8-bit form (codes, scale) of a merged layer, or of one without an adapter (see qalora_deploy_int8)."""
+    _need(packed, "packed", nbytes=packed_bytes(desc))
+    dev = packed.device
+    L = desc.d_in // max(desc.group, 1)
+    if check_desc(desc) == OK:
+        _need(alpha, "alpha", torch.float32, (L, desc.d_out), device=dev)
+        _need(beta, "beta", torch.float32, (L, desc.d_out), device=dev)
+    codes = torch.empty((max(desc.d_out, 0), max(desc.d_in, 0)), dtype=torch.int8, device=dev)
+    scale = torch.empty(max(desc.d_out, 0), dtype=torch.float32, device=dev)
+    with _on(dev):
+        rc = load().qalora_deploy_int8(ctypes.byref(desc), _p(packed), _p(alpha), _p(beta), _p(codes), _p(scale), _stream())
+    _check(rc, "qalora_deploy_int8")
+    return codes, scale
+
+
+def _matrix(t, name, dtype):
+    _need(t, name, dtype)
+    if t.dim() != 2:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected a matrix")
+    return t.shape[0], t.shape[1], t.device
+
+
+def _given(t, name, dtype, shape, dev):
+    """An output: the caller's, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    _need(t, name, dtype, shape, device=dev)
+    return t
+
+
+def quantize_tokens(x, factor=None, q=None, s=None):
+    """x bf16 [tokens, cols], each row in 8 bits with a scale of its own: (q int8 [tokens, cols], s fp32 [tokens]), what
+    forward_int8 takes in place of x.  ``factor`` fp32 [cols] multiplies the columns first."""
+    T, cols, dev = _matrix(x, "x", torch.bfloat16)
+    _need(factor, "factor", torch.float32, (cols,), device=dev, optional=True)
+    q, s = _given(q, "q", torch.int8, (T, cols), dev), _given(s, "s", torch.float32, (T,), dev)
+    with _on(dev):
+        rc = load().qalora_quantize_tokens(T, cols, _p(x), _p(factor), _p(q), _p(s), _stream())
+    _check(rc, "qalora_quantize_tokens")
+    return q, s
+
+
+def int8_workspace_bytes(tokens: int, d_in: int, d_out: int, op: int) -> int:
+    """Workspace of forward_int8 (OP_FORWARD) and backward_int8 (OP_BACKWARD) for up to so many tokens."""
+    return int(load().qalora_int8_workspace_bytes(int(tokens), int(d_in), int(d_out), int(op)))
+
+
+def _int8_workspace(T, d_in, d_out, op, ws, dev):
+    if ws is None:
+        ws = torch.empty(max(int8_workspace_bytes(T, d_in, d_out, op), 16), dtype=torch.uint8, device=dev)
+    _need(ws, "ws", device=dev)
+    return ws, ws.numel() * ws.element_size()
+
+
+def forward_int8(x, codes, scale, bias=None, act="none", mul=None, residual=None, keep_z=False, out_dtype=torch.float32, ws=None,
+                 y=None, z=None):
+    """y = act(s (q codes^T) scale + bias) * mul + residual in 8-bit integers (see qalora_forward_int8).  ``x`` is bf16
+    [tokens, d_in], or what quantize_tokens or swiglu_forward_int8 made of one: (q, s).  The epilogue is forward_epilogue's.
+    Returns y, or with ``keep_z`` (y, z)."""
+    d_out, d_in, dev = _matrix(codes, "codes", torch.int8)
+    _need(scale, "scale", torch.float32, (d_out,), device=dev)
+    s = None
+    if isinstance(x, (tuple, list)):
+        x, s = x
+        _need(x, "x", torch.int8, device=dev)
+    else:
+        _need(x, "x", torch.bfloat16, device=dev)
+    if x.dim() != 2 or x.shape[1] != d_in:
+        raise ValueError(f"x: shape {tuple(x.shape)}, expected [tokens, {d_in}]")
+    if x.dtype == torch.int8:
+        _need(s, "x's scales", torch.float32, (x.shape[0],), device=dev)
+    T = x.shape[0]
+    if y is None:
+        y = torch.empty((T, d_out), dtype=out_dtype, device=dev)
+    _need_out(y, "y", T, d_out, dev)
+    if z is not None and not keep_z:
+        raise ValueError("z: given without keep_z")
+    if keep_z and z is None:
+        z = torch.empty((T, d_out), dtype=torch.bfloat16, device=dev)
+    epi = _epilogue(T, d_out, dev, y, bias, act, mul, residual, z)
+    ws, ws_bytes = _int8_workspace(T, d_in, d_out, OP_FORWARD, ws, dev)
+    with _on(dev):
+        rc = load().qalora_forward_int8(T, d_in, d_out, _p(x), _p(s), _p(codes), _p(scale), ctypes.byref(epi), _p(y),
+                                        BF16 if y.dtype == torch.bfloat16 else F32, _p(ws), ws_bytes, _stream())
+    _check(rc, "qalora_forward_int8")
+    return (y, z) if keep_z else y
+
+
+def backward_int8(dy, codes, scale, residual=None, dx_dtype=torch.float32, ws=None, dx=None):
+    """dx of forward_int8's product with the weight frozen (see qalora_backward_int8): dy bf16 [tokens, d_out] -> dx [tokens, d_in],
+    plus ``residual`` (dx's type; it may be the ``dx`` that is passed: gradients of several linears then add up in place)."""
+    d_out, d_in, dev = _matrix(codes, "codes", torch.int8)
+    _need(scale, "scale", torch.float32, (d_out,), device=dev)
+    _need(dy, "dy", torch.bfloat16, device=dev)
+    if dy.dim() != 2 or dy.shape[1] != d_out:
+        raise ValueError(f"dy: shape {tuple(dy.shape)}, expected [tokens, {d_out}]")
+    T = dy.shape[0]
+    if dx is None:
+        dx = torch.empty((T, d_in), dtype=dx_dtype, device=dev)
+    _need_out(dx, "dx", T, d_in, dev)
+    _need(residual, "residual", dx.dtype, (T, d_in), device=dev, optional=True)
+    ws, ws_bytes = _int8_workspace(T, d_in, d_out, OP_BACKWARD, ws, dev)
+    with _on(dev):
+        rc = load().qalora_backward_int8(T, d_in, d_out, _p(dy), _p(codes), _p(scale), _p(residual), _p(dx),
+                                         BF16 if dx.dtype == torch.bfloat16 else F32, _p(ws), ws_bytes, _stream())
+    _check(rc, "qalora_backward_int8")
+    return dx
+
+
+def kept8_bytes(tokens: int, cols: int) -> int:
+    return int(load().qalora_kept8_bytes(int(tokens), int(cols)))
+
+
+def _kept8(kept, name, tokens, cols, dev, new=False):
+    n = kept8_bytes(tokens, cols)
+    if kept is None and new:
+        return torch.empty(max(n, 16), dtype=torch.uint8, device=dev)
+    _need(kept, name, torch.uint8, nbytes=n, device=dev)
+    return kept
+
+
+def keep8(x, kept=None):
+    """x bf16 [tokens, cols] kept in 8 bits for a backward (see qalora_keep8): an opaque uint8 tensor."""
+    T, cols, dev = _matrix(x, "x", torch.bfloat16)
+    kept = _kept8(kept, "kept", T, cols, dev, new=True)
+    with _on(dev):
+        rc = load().qalora_keep8(T, cols, _p(x), _p(kept), _stream())
+    _check(rc, "qalora_keep8")
+    return kept
+
+
+def restore8(kept, tokens, cols, x=None):
+    """What keep8 (or, with twice the tokens, swiglu_forward_keep8) kept, as bf16 [tokens, cols]."""
+    _need(kept, "kept", torch.uint8, nbytes=kept8_bytes(tokens, cols))
+    x = _given(x, "x", torch.bfloat16, (tokens, cols), kept.device)
+    with _on(kept.device):
+        rc = load().qalora_restore8(tokens, cols, _p(kept), _p(x), _stream())
+    _check(rc, "qalora_restore8")
+    return x
+
+
+def _swiglu_input(gu, cols):
+    T, width, dev = _matrix(gu, "gu", torch.bfloat16)
+    if width != 2 * cols:
+        raise ValueError(f"gu: shape {tuple(gu.shape)}, expected [tokens, {2 * cols}]")
+    return T, dev
+
+
+def swiglu_forward_keep8(gu, cols, h=None, kept=None):
+    """h = silu(gate) * up of gu = [gate | up] (bf16 [tokens, 2 cols]), and gate and up kept in 8 bits: (h, kept)."""
+    T, dev = _swiglu_input(gu, cols)
+    h = _given(h, "h", torch.bfloat16, (T, cols), dev)
+    kept = _kept8(kept, "kept", 2 * T, cols, dev, new=True)
+    with _on(dev):
+        rc = load().qalora_swiglu_forward8(T, cols, _p(gu), _p(h), None, None, _p(kept), _stream())
+    _check(rc, "qalora_swiglu_forward8")
+    return h, kept
+
+
+def swiglu_forward_int8(gu, cols, keep=False, q=None, s=None, kept=None, h=None):
+    """silu(gate) * up of gu = [gate | up] as 8-bit tokens (q, s), what forward_int8 of the down projection takes; with
+    ``keep`` ((q, s), kept), gate and up kept in 8 bits as by swiglu_forward_keep8.  A given ``h`` receives the hidden activations."""
+    T, dev = _swiglu_input(gu, cols)
+    q, s = _given(q, "q", torch.int8, (T, cols), dev), _given(s, "s", torch.float32, (T,), dev)
+    _need(h, "h", torch.bfloat16, (T, cols), device=dev, optional=True)
+    if kept is not None and not keep:
+        raise ValueError("kept: given without keep")
+    if keep:
+        kept = _kept8(kept, "kept", 2 * T, cols, dev, new=True)
+    with _on(dev):
+        rc = load().qalora_swiglu_forward8(T, cols, _p(gu), _p(h), _p(q), _p(s), _p(kept), _stream())
+    _check(rc, "qalora_swiglu_forward8")
+    return ((q, s), kept) if keep else (q, s)
+
+
+def swiglu_backward_kept8(dh, kept, cols, dgu=None):
+    """dgu = [dgate | dup] from dh (bf16 [tokens, cols]) and the gate and up that were kept in 8 bits."""
+    T, width, dev = _matrix(dh, "dh", torch.bfloat16)
+    if width != cols:
+        raise ValueError(f"dh: shape {tuple(dh.shape)}, expected [tokens, {cols}]")
+    _kept8(kept, "kept", 2 * T, cols, dev)
+    dgu = _given(dgu, "dgu", torch.bfloat16, (T, 2 * cols), dev)
+    with _on(dev):
+        rc = load().qalora_swiglu_backward_kept8(T, cols, _p(dh), _p(kept), _p(dgu), _stream())
+    _check(rc, "qalora_swiglu_backward_kept8")
+    return dgu
+
+
+def epilogue_backward_kept8(dy, z8=None, act="none", mul8=None, want_dz=True, want_dbias=False, dz=None, dmul=None, dbias=None,
+                            accumulate=False, ws=None):
+    """epilogue_backward with z and mul as keep8 kept them: (dz, dmul, dbias), None in the place of what is not there."""
+    _need(dy, "dy")
+    if dy.dim() != 2 or dy.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"dy: {dy.dtype} {tuple(dy.shape)}, expected a float32 or bfloat16 matrix")
+    (T, cols), dev = dy.shape, dy.device
+    if z8 is not None:
+        _kept8(z8, "z8", T, cols, dev)
+    if mul8 is not None:
+        _kept8(mul8, "mul8", T, cols, dev)
+    if dmul is not None and mul8 is None:
+        raise ValueError("dmul: given without mul8")
+    if want_dz or dz is not None:
+        dz = _given(dz, "dz", torch.bfloat16, (T, cols), dev)
+    if mul8 is not None:
+        dmul = _given(dmul, "dmul", torch.bfloat16, (T, cols), dev)
+    if want_dbias and dbias is None:
+        dbias = torch.zeros(cols, dtype=torch.float32, device=dev)
+    _need(dbias, "dbias", torch.float32, (cols,), device=dev, optional=True)
+    if ws is None and dbias is not None:
+        n = int(load().qalora_epilogue_backward_workspace_bytes(T, cols))
+        ws = torch.empty(max(n, 16), dtype=torch.uint8, device=dev)
+    _need(ws, "ws", device=dev, optional=True)
+    act = _act(act)
+    with _on(dev):
+        rc = load().qalora_epilogue_backward_kept8(act, T, cols, _p(dy), BF16 if dy.dtype == torch.bfloat16 else F32, _p(z8),
+                                                   _p(mul8), _p(dz), _p(dmul), _p(dbias), 1 if accumulate else 0, _p(ws),
+                                                   0 if ws is None else ws.numel() * ws.element_size(), _stream())
+    _check(rc, "qalora_epilogue_backward_kept8")
+    return dz, dmul, dbias
 
 
 class KernelTimer:

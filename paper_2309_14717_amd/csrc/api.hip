@@ -6,9 +6,11 @@
 #include "gemm_plan.hpp"
 #include "kernels.hpp"
 #include "midt_plan.hpp"
+#include "tokens8_plan.hpp"
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 using namespace qalora;
 
@@ -555,11 +557,11 @@ static int forward_mid(const qalora_desc& d, int tokens, const void* x, const vo
 }
 
 // Whether an output of a forward with an epilogue lies over an operand that is still read, or over another output.
-static bool epilogue_overlaps(const qalora_desc& d, int tokens, const void* x, const Epilogue& e, const void* y, int y_dtype,
-                              const void* kept) {
-  const size_t n = (size_t)tokens * d.d_out, y_bytes = n * (y_dtype == QALORA_BF16 ? 2 : 4);
-  const Span out[3] = {{y, y_bytes}, {e.z, 2 * n}, {kept, kept ? qalora_kept_bytes(&d, tokens) : 0}};
-  const Span in[2] = {{x, 2 * (size_t)tokens * d.d_in}, {e.bias, sizeof(float) * d.d_out}};
+static bool epilogue_overlaps(int tokens, int d_out, const Span& x, const Epilogue& e, const void* y, int y_dtype,
+                              const Span& kept) {
+  const size_t n = (size_t)tokens * d_out, y_bytes = n * (y_dtype == QALORA_BF16 ? 2 : 4);
+  const Span out[3] = {{y, y_bytes}, {e.z, 2 * n}, kept};
+  const Span in[2] = {x, {e.bias, sizeof(float) * d_out}};
   const Span at_y[2] = {{e.mul, 2 * n}, {e.residual, y_bytes}};  // an element of these is read only for y's of the same place
   for (int i = 0; i < 3; ++i) {
     for (const Span& s : in)
@@ -570,6 +572,12 @@ static bool epilogue_overlaps(const qalora_desc& d, int tokens, const void* x, c
       if (overlap(out[i], out[k])) return true;
   }
   return false;
+}
+
+static bool epilogue_overlaps(const qalora_desc& d, int tokens, const void* x, const Epilogue& e, const void* y, int y_dtype,
+                              const void* kept) {
+  return epilogue_overlaps(tokens, d.d_out, {x, 2 * (size_t)tokens * d.d_in}, e, y, y_dtype,
+                           {kept, kept ? qalora_kept_bytes(&d, tokens) : 0});
 }
 
 static int forward_impl(const qalora_desc* d, int tokens, const void* x, const void* packed,
@@ -711,8 +719,10 @@ size_t qalora_epilogue_backward_workspace_bytes(int tokens, int cols) {
   return align_up(epilogue_back_floats(tokens, cols) * sizeof(float));
 }
 
-int qalora_epilogue_backward(int act, int tokens, int cols, const void* dy, int dy_dtype, const void* z, const void* mul,
-                             void* dz, void* dmul, float* dbias, int accumulate, void* ws, size_t ws_bytes, void* stream) {
+// `kept8`: z and mul are as qalora_keep8 left them.
+static int epilogue_backward_impl(int act, int tokens, int cols, const void* dy, int dy_dtype, const void* z, const void* mul,
+                                  bool kept8, void* dz, void* dmul, float* dbias, int accumulate, void* ws, size_t ws_bytes,
+                                  void* stream) {
   if (act < QALORA_ACT_NONE || act > QALORA_ACT_GELU_TANH || tokens <= 0 || cols <= 0 || !dy) return QALORA_EINVAL;
   if (dy_dtype != QALORA_F32 && dy_dtype != QALORA_BF16) return QALORA_EINVAL;
   if (accumulate != 0 && accumulate != 1) return QALORA_EINVAL;
@@ -726,15 +736,24 @@ int qalora_epilogue_backward(int act, int tokens, int cols, const void* dy, int 
   const size_t need = dbias ? epilogue_back_floats(tokens, cols) * sizeof(float) : 0;
   if (need > 0 && (!ws || ws_bytes < need)) return QALORA_EWORKSPACE;
   const size_t n = (size_t)tokens * cols;
-  const Span in[3] = {{dy, n * (dy_dtype == QALORA_BF16 ? 2 : 4)}, {z, 2 * n}, {mul, 2 * n}};
+  const size_t operand = kept8 ? keep8_bytes(tokens, cols) : 2 * n;
+  const Span in[3] = {{dy, n * (dy_dtype == QALORA_BF16 ? 2 : 4)}, {z, operand}, {mul, operand}};
   const Span o_dz{dz, 2 * n}, o_dmul{dmul, 2 * n}, o_dbias{dbias, sizeof(float) * cols};
   if (overlap(o_dz, o_dmul) || overlap(o_dbias, o_dz) || overlap(o_dbias, o_dmul)) return QALORA_EINVAL;
   for (const Span& i : in)
     if (spoils(o_dz, i) || spoils(o_dmul, i) || overlap(o_dbias, i)) return QALORA_EINVAL;
+  if (kept8)
+    for (const Span& i : {in[1], in[2]})  // (whatever their sizes: codes do not lie where a thread's own elements do)
+      if (overlap(o_dz, i) || overlap(o_dmul, i)) return QALORA_EINVAL;
   EpilogueBackArgs a{};
   a.dy = dy;
-  a.z = static_cast<const uint16_t*>(z);
-  a.mul = static_cast<const uint16_t*>(mul);
+  if (kept8) {
+    a.z8 = static_cast<const uint8_t*>(z);
+    a.mul8 = static_cast<const uint8_t*>(mul);
+  } else {
+    a.z = static_cast<const uint16_t*>(z);
+    a.mul = static_cast<const uint16_t*>(mul);
+  }
   a.dz = static_cast<uint16_t*>(dz);
   a.dmul = static_cast<uint16_t*>(dmul);
   a.dbias = dbias;
@@ -745,6 +764,278 @@ int qalora_epilogue_backward(int act, int tokens, int cols, const void* dy, int 
   a.rows = tokens;
   a.cols = cols;
   return launch_epilogue_backward(a, as_stream(stream)) == hipSuccess ? QALORA_OK : QALORA_EHIP;
+}
+
+int qalora_epilogue_backward(int act, int tokens, int cols, const void* dy, int dy_dtype, const void* z, const void* mul,
+                             void* dz, void* dmul, float* dbias, int accumulate, void* ws, size_t ws_bytes, void* stream) {
+  return epilogue_backward_impl(act, tokens, cols, dy, dy_dtype, z, mul, false, dz, dmul, dbias, accumulate, ws, ws_bytes, stream);
+}
+
+// ---- 8-bit integers ------------------------------------------------------------------------------------------------------
+static_assert(T8_MAX_COLS == QALORA_INT8_MAX_SIDE, "the header documents this limit");
+
+static int int8_sizes(int d_in, int d_out) {
+  if (d_in <= 0 || d_out <= 0) return QALORA_EINVAL;
+  if (d_in % 16 != 0 || d_out % 8 != 0 || d_in > QALORA_INT8_MAX_SIDE || d_out > QALORA_INT8_MAX_SIDE) return QALORA_EUNSUPPORTED;
+  return QALORA_OK;
+}
+static bool any_overlap(const Span& out, std::initializer_list<Span> in) {
+  for (const Span& i : in)
+    if (overlap(out, i)) return true;
+  return false;
+}
+
+int qalora_quantize_int8(int d_in, int d_out, const float* W, int8_t* codes, float* scale, void* stream) {
+  if (!W || !codes || !scale) return QALORA_EINVAL;
+  if (const int rc = int8_sizes(d_in, d_out); rc != QALORA_OK) return rc;
+  if (misaligned(W) || misaligned(codes) || misaligned(scale)) return QALORA_EALIGN;
+  const size_t n = (size_t)d_in * d_out;
+  const Span w{W, 4 * n}, c{codes, n}, s{scale, sizeof(float) * d_out};
+  if (any_overlap(c, {w, s}) || overlap(s, w)) return QALORA_EINVAL;
+  Weight8Args a{};
+  a.W = W;
+  a.codes = codes;
+  a.scale = scale;
+  a.d_in = d_in;
+  a.d_out = d_out;
+  return launch_weight8(a, as_stream(stream)) == hipSuccess ? QALORA_OK : QALORA_EHIP;
+}
+
+int qalora_deploy_int8(const qalora_desc* d, const void* packed, const float* alpha, const float* beta, int8_t* codes,
+                       float* scale, void* stream) {
+  if (const int rc = qalora_check_desc(d); rc != QALORA_OK) return rc;
+  if (!packed || !alpha || !beta || !codes || !scale) return QALORA_EINVAL;
+  if (const int rc = int8_sizes(d->d_in, d->d_out); rc != QALORA_OK) return rc;
+  if (misaligned(packed) || misaligned(alpha) || misaligned(beta) || misaligned(codes) || misaligned(scale)) return QALORA_EALIGN;
+  const size_t factors = sizeof(float) * (size_t)(d->d_in / d->group) * d->d_out;
+  const Span p{packed, qalora_packed_bytes(d)}, al{alpha, factors}, be{beta, factors}, c{codes, (size_t)d->d_in * d->d_out},
+      s{scale, sizeof(float) * d->d_out};
+  if (any_overlap(c, {p, al, be, s}) || any_overlap(s, {p, al, be})) return QALORA_EINVAL;
+  Weight8Args a{};
+  a.plane0 = static_cast<const uint32_t*>(packed);
+  a.plane1 = a.plane0 + plane0_words(d->bits, d->d_in, d->d_out);
+  a.alpha = alpha;
+  a.beta = beta;
+  a.codes = codes;
+  a.scale = scale;
+  a.d_in = d->d_in;
+  a.d_out = d->d_out;
+  a.group = d->group;
+  a.bits = d->bits;
+  return launch_weight8(a, as_stream(stream)) == hipSuccess ? QALORA_OK : QALORA_EHIP;
+}
+
+int qalora_quantize_tokens(int tokens, int cols, const void* x, const float* factor, int8_t* q, float* s, void* stream) {
+  if (tokens <= 0 || cols <= 0 || !x || !q || !s) return QALORA_EINVAL;
+  if (cols % 8 != 0 || cols > QALORA_INT8_MAX_SIDE) return QALORA_EUNSUPPORTED;
+  if (misaligned(x) || misaligned(factor) || misaligned(q) || misaligned(s)) return QALORA_EALIGN;
+  const size_t n = (size_t)tokens * cols;
+  const Span in{x, 2 * n}, f{factor, sizeof(float) * cols}, codes{q, n}, scales{s, sizeof(float) * (size_t)tokens};
+  if (any_overlap(codes, {in, f, scales}) || any_overlap(scales, {in, f})) return QALORA_EINVAL;
+  Tokens8Args a{};
+  a.x = x;
+  a.factor = factor;
+  a.codes = q;
+  a.scale = s;
+  a.rows = tokens;
+  a.cols = a.ld = cols;
+  a.from = factor ? TOKENS8_SCALED : TOKENS8_PLAIN;
+  return launch_tokens8(a, as_stream(stream)) == hipSuccess ? QALORA_OK : QALORA_EHIP;
+}
+
+// Workspace of the products: the codes and scales of the tokens (rows of whole 16 bytes).
+struct Int8Plan {
+  size_t q, s, total;
+  int ld;
+};
+static Int8Plan plan_int8(int tokens, int K) {
+  Int8Plan p{};
+  Carver c;
+  p.ld = round_up(K, 16);
+  p.s = c.take(sizeof(float) * (size_t)tokens);
+  p.q = c.take((size_t)tokens * p.ld);
+  p.total = c.off;
+  return p;
+}
+size_t qalora_int8_workspace_bytes(int tokens, int d_in, int d_out, int op) {
+  if (tokens <= 0 || int8_sizes(d_in, d_out) != QALORA_OK || (op != QALORA_OP_FORWARD && op != QALORA_OP_BACKWARD)) return 0;
+  return plan_int8(tokens, op == QALORA_OP_FORWARD ? d_in : d_out).total;
+}
+
+int qalora_forward_int8(int tokens, int d_in, int d_out, const void* x, const float* x_scale, const int8_t* codes,
+                        const float* scale, const qalora_epilogue* epilogue, void* y, int y_dtype, void* ws, size_t ws_bytes,
+                        void* stream) {
+  if (tokens <= 0 || !x || !codes || !scale || !y) return QALORA_EINVAL;
+  if (y_dtype != QALORA_F32 && y_dtype != QALORA_BF16) return QALORA_EINVAL;
+  if (const int rc = int8_sizes(d_in, d_out); rc != QALORA_OK) return rc;
+  Epilogue e{};
+  const Epilogue* use;
+  if (const int rc = read_epilogue(epilogue, y, e, &use); rc != QALORA_OK) return rc;
+  if (misaligned(x) || misaligned(x_scale) || misaligned(codes) || misaligned(scale) || misaligned(y) || misaligned(ws))
+    return QALORA_EALIGN;
+  const Int8Plan plan = plan_int8(tokens, d_in);
+  if (!ws || ws_bytes < plan.total) return QALORA_EWORKSPACE;
+  const size_t n = (size_t)tokens * d_out;
+  const Span weights{codes, (size_t)d_in * d_out}, scales{scale, sizeof(float) * d_out},
+      x_scales{x_scale, sizeof(float) * (size_t)tokens};
+  if (epilogue_overlaps(tokens, d_out, {x, (x_scale ? 1 : 2) * (size_t)tokens * d_in}, e, y, y_dtype, {nullptr, 0}) ||
+      any_overlap({y, n * (y_dtype == QALORA_BF16 ? 2 : 4)}, {weights, scales, x_scales}) ||
+      any_overlap({e.z, 2 * n}, {weights, scales, x_scales}))
+    return QALORA_EINVAL;
+  char* w = static_cast<char*>(ws);
+  Int8GemmArgs g{};
+  if (x_scale) {
+    g.tokens = static_cast<const int8_t*>(x);
+    g.row_scale = x_scale;
+    g.lda = d_in;
+  } else {
+    Tokens8Args a{};
+    a.x = x;
+    a.codes = reinterpret_cast<int8_t*>(w + plan.q);
+    a.scale = reinterpret_cast<float*>(w + plan.s);
+    a.rows = tokens;
+    a.cols = d_in;
+    a.ld = plan.ld;
+    a.from = TOKENS8_PLAIN;
+    if (launch_tokens8(a, as_stream(stream)) != hipSuccess) return QALORA_EHIP;
+    g.tokens = a.codes;
+    g.row_scale = a.scale;
+    g.lda = plan.ld;
+  }
+  g.codes = codes;
+  g.col_scale = scale;
+  g.out = y;
+  g.out_bf16 = y_dtype == QALORA_BF16;
+  g.epi = e;
+  g.M = tokens;
+  g.N = d_out;
+  g.K = d_in;
+  return launch_gemm_i8(g, as_stream(stream)) == hipSuccess ? QALORA_OK : QALORA_EHIP;
+}
+
+int qalora_backward_int8(int tokens, int d_in, int d_out, const void* dy, const int8_t* codes, const float* scale,
+                         const void* residual, void* dx, int dx_dtype, void* ws, size_t ws_bytes, void* stream) {
+  if (tokens <= 0 || !dy || !codes || !scale || !dx) return QALORA_EINVAL;
+  if (dx_dtype != QALORA_F32 && dx_dtype != QALORA_BF16) return QALORA_EINVAL;
+  if (const int rc = int8_sizes(d_in, d_out); rc != QALORA_OK) return rc;
+  if (misaligned(dy) || misaligned(codes) || misaligned(scale) || misaligned(residual) || misaligned(dx) || misaligned(ws))
+    return QALORA_EALIGN;
+  const Int8Plan plan = plan_int8(tokens, d_out);
+  if (!ws || ws_bytes < plan.total) return QALORA_EWORKSPACE;
+  const Span out{dx, (size_t)tokens * d_in * (dx_dtype == QALORA_BF16 ? 2 : 4)};
+  if (any_overlap(out, {{dy, 2 * (size_t)tokens * d_out}, {codes, (size_t)d_in * d_out}, {scale, sizeof(float) * d_out}}) ||
+      spoils(out, {residual, out.bytes}))
+    return QALORA_EINVAL;
+  char* w = static_cast<char*>(ws);
+  Tokens8Args a{};
+  a.x = dy;
+  a.factor = scale;
+  a.codes = reinterpret_cast<int8_t*>(w + plan.q);
+  a.scale = reinterpret_cast<float*>(w + plan.s);
+  a.rows = tokens;
+  a.cols = d_out;
+  a.ld = plan.ld;
+  a.from = TOKENS8_SCALED;
+  if (launch_tokens8(a, as_stream(stream)) != hipSuccess) return QALORA_EHIP;
+  Int8GemmArgs g{};
+  g.tokens = a.codes;
+  g.row_scale = a.scale;
+  g.lda = plan.ld;
+  g.codes = codes;
+  g.out = dx;
+  g.out_bf16 = dx_dtype == QALORA_BF16;
+  g.epi.residual = residual;
+  g.epi.on = residual != nullptr;
+  g.back = 1;
+  g.M = tokens;
+  g.N = d_in;
+  g.K = d_out;
+  return launch_gemm_i8(g, as_stream(stream)) == hipSuccess ? QALORA_OK : QALORA_EHIP;
+}
+
+// ---- activations kept in 8 bits --------------------------------------------------------------------------------------------
+static bool keepable(int tokens, int cols) { return tokens > 0 && cols > 0 && cols % 8 == 0 && cols <= EB_MAX_COLS; }
+
+size_t qalora_kept8_bytes(int tokens, int cols) { return keepable(tokens, cols) ? keep8_bytes(tokens, cols) : 0; }
+
+static int keep8_call(int tokens, int cols, const void* x, const void* kept, Keep8Args& a) {
+  if (tokens <= 0 || cols <= 0 || !x || !kept) return QALORA_EINVAL;
+  if (misaligned(x) || misaligned(kept)) return QALORA_EALIGN;
+  if (!keepable(tokens, cols)) return QALORA_EUNSUPPORTED;
+  if (overlap({x, 2 * (size_t)tokens * cols}, {kept, keep8_bytes(tokens, cols)})) return QALORA_EINVAL;
+  a.x = static_cast<uint16_t*>(const_cast<void*>(x));
+  a.kept = static_cast<uint8_t*>(const_cast<void*>(kept));
+  a.rows = tokens;
+  a.cols = cols;
+  return QALORA_OK;
+}
+int qalora_keep8(int tokens, int cols, const void* x, void* kept, void* stream) {
+  Keep8Args a{};
+  if (const int rc = keep8_call(tokens, cols, x, kept, a); rc != QALORA_OK) return rc;
+  return launch_keep8(a, as_stream(stream)) == hipSuccess ? QALORA_OK : QALORA_EHIP;
+}
+int qalora_restore8(int tokens, int cols, const void* kept, void* x, void* stream) {
+  Keep8Args a{};
+  if (const int rc = keep8_call(tokens, cols, x, kept, a); rc != QALORA_OK) return rc;
+  return launch_restore8(a, as_stream(stream)) == hipSuccess ? QALORA_OK : QALORA_EHIP;
+}
+
+int qalora_swiglu_forward8(int tokens, int cols, const void* gu, void* h, int8_t* q, float* s, void* kept, void* stream) {
+  if (tokens <= 0 || cols <= 0 || !gu || (!h && !q && !kept) || (q == nullptr) != (s == nullptr)) return QALORA_EINVAL;
+  if (misaligned(gu) || misaligned(h) || misaligned(q) || misaligned(s) || misaligned(kept)) return QALORA_EALIGN;
+  if (!keepable(tokens, cols) || tokens >= 1 << 30 || (q && cols > QALORA_INT8_MAX_SIDE)) return QALORA_EUNSUPPORTED;
+  const size_t n = (size_t)tokens * cols;
+  const Span in{gu, 4 * n}, out[4] = {{h, 2 * n}, {q, n}, {s, sizeof(float) * (size_t)tokens}, {kept, keep8_bytes(2 * (size_t)tokens, cols)}};
+  for (int i = 0; i < 4; ++i) {
+    if (overlap(out[i], in)) return QALORA_EINVAL;
+    for (int k = 0; k < i; ++k)
+      if (overlap(out[i], out[k])) return QALORA_EINVAL;
+  }
+  hipError_t e;
+  if (q) {
+    Tokens8Args a{};
+    a.x = gu;
+    a.codes = q;
+    a.scale = s;
+    a.h = static_cast<uint16_t*>(h);
+    a.kept = static_cast<uint8_t*>(kept);
+    a.rows = tokens;
+    a.cols = a.ld = cols;
+    a.from = TOKENS8_SWIGLU;
+    e = launch_tokens8(a, as_stream(stream));
+  } else if (kept) {
+    Swiglu8Args a{};
+    a.gu = static_cast<uint16_t*>(const_cast<void*>(gu));
+    a.h = static_cast<uint16_t*>(h);
+    a.kept = static_cast<uint8_t*>(kept);
+    a.rows = tokens;
+    a.cols = cols;
+    e = launch_swiglu_keep8(a, as_stream(stream));
+  } else {
+    e = launch_swiglu_forward_wide(gu, h, tokens, cols, as_stream(stream));
+  }
+  return e == hipSuccess ? QALORA_OK : QALORA_EHIP;
+}
+
+int qalora_swiglu_backward_kept8(int tokens, int cols, const void* dh, const void* kept, void* dgu, void* stream) {
+  if (tokens <= 0 || cols <= 0 || !dh || !kept || !dgu) return QALORA_EINVAL;
+  if (misaligned(dh) || misaligned(kept) || misaligned(dgu)) return QALORA_EALIGN;
+  if (!keepable(tokens, cols) || tokens >= 1 << 30) return QALORA_EUNSUPPORTED;
+  const size_t n = (size_t)tokens * cols;
+  if (any_overlap({dgu, 4 * n}, {{dh, 2 * n}, {kept, keep8_bytes(2 * (size_t)tokens, cols)}})) return QALORA_EINVAL;
+  Swiglu8Args a{};
+  a.gu = static_cast<uint16_t*>(dgu);
+  a.h = static_cast<uint16_t*>(const_cast<void*>(dh));
+  a.kept = static_cast<uint8_t*>(const_cast<void*>(kept));
+  a.rows = tokens;
+  a.cols = cols;
+  return launch_swiglu_kept8_backward(a, as_stream(stream)) == hipSuccess ? QALORA_OK : QALORA_EHIP;
+}
+
+int qalora_epilogue_backward_kept8(int act, int tokens, int cols, const void* dy, int dy_dtype, const void* z8, const void* mul8,
+                                   void* dz, void* dmul, float* dbias, int accumulate, void* ws, size_t ws_bytes, void* stream) {
+  if (!z8 && !mul8) return QALORA_EINVAL;
+  return epilogue_backward_impl(act, tokens, cols, dy, dy_dtype, z8, mul8, true, dz, dmul, dbias, accumulate, ws, ws_bytes, stream);
 }
 
 static int backward_impl(const qalora_desc* d, int tokens, const void* dy, const void* x,

@@ -4,6 +4,7 @@
 // what the linear's backward takes as its dy, in bf16 as there; dbias is the sum of the unrounded fp32 values, each
 // block's rows first, then the blocks in order (a second small launch): no atomics, reruns are bit-identical.
 #include "epilogue.hpp"
+#include "int8.hpp"
 #include "kernels.hpp"
 
 namespace qalora {
@@ -20,7 +21,8 @@ __device__ __forceinline__ u32x4 pack8(const float (&f)[8]) {
 }
 }  // namespace
 
-template <bool DY_BF16>
+// KEPT8: z and mul as they were kept in 8 bits (int8.hpp): one byte a column of each, and one more for 32
+template <bool DY_BF16, bool KEPT8>
 __global__ __launch_bounds__(EB_THREADS) void epilogue_back_kernel(const EpilogueBackArgs p) {
   __shared__ float share[EB_THREADS][8 + 1];
   const int lane = threadIdx.x & (p.plan.lanes - 1), row_in = threadIdx.x / p.plan.lanes;
@@ -42,8 +44,18 @@ __global__ __launch_bounds__(EB_THREADS) void epilogue_back_kernel(const Epilogu
       w.dy[0] = src[0];
       w.dy[1] = src[1];
     }
-    if (p.z) w.z = *reinterpret_cast<const u32x4*>(p.z + at);
-    if (p.mul) w.mul = *reinterpret_cast<const u32x4*>(p.mul + at);
+    if constexpr (KEPT8) {
+      const size_t e = keep8_exponents_at(p.rows, p.cols) + (size_t)r * keep8_groups(p.cols) + col / kKeepGroup;
+      auto load8 = [&](const uint8_t* kept) {
+        const u8x8 c = *reinterpret_cast<const u8x8*>(kept + at);
+        return u32x4{c[0], c[1], kept[e], 0};
+      };
+      if (p.z8) w.z = load8(p.z8);
+      if (p.mul8) w.mul = load8(p.mul8);
+    } else {
+      if (p.z) w.z = *reinterpret_cast<const u32x4*>(p.z + at);
+      if (p.mul) w.mul = *reinterpret_cast<const u32x4*>(p.mul + at);
+    }
     return w;
   };
   if (live && r0 + row_in < r1) {
@@ -59,8 +71,13 @@ __global__ __launch_bounds__(EB_THREADS) void epilogue_back_kernel(const Epilogu
 #pragma unroll
         for (int k = 0; k < 8; ++k) dy[k] = __uint_as_float(w.dy[k >> 2][k & 3]);
       }
-      unpack8(w.z, z);
-      unpack8(w.mul, mul);
+      if constexpr (KEPT8) {
+        restore8(u8x8{w.z[0], w.z[1]}, w.z[2], z);
+        restore8(u8x8{w.mul[0], w.mul[1]}, w.mul[2], mul);
+      } else {
+        unpack8(w.z, z);
+        unpack8(w.mul, mul);
+      }
       float dz[8], dmul[8];
       with_act(p.act, [&](auto act) {
 #pragma unroll
@@ -73,7 +90,7 @@ __global__ __launch_bounds__(EB_THREADS) void epilogue_back_kernel(const Epilogu
       });
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        if (p.mul) dz[k] *= mul[k];
+        if (KEPT8 ? p.mul8 != nullptr : p.mul != nullptr) dz[k] *= mul[k];
         sum[k] += dz[k];
       }
       if (p.dz) *reinterpret_cast<u32x4*>(p.dz + at) = pack8(dz);
@@ -118,8 +135,10 @@ hipError_t launch_epilogue_backward(const EpilogueBackArgs& args, hipStream_t st
   EpilogueBackArgs a = args;
   a.plan = epilogue_back_plan(a.rows, a.cols);
   const dim3 grid(a.plan.col_blocks, a.plan.row_blocks);
-  if (a.dy_bf16) epilogue_back_kernel<true><<<grid, EB_THREADS, 0, st>>>(a);
-  else epilogue_back_kernel<false><<<grid, EB_THREADS, 0, st>>>(a);
+  const bool kept8 = a.z8 || a.mul8;
+  auto kernel = a.dy_bf16 ? (kept8 ? epilogue_back_kernel<true, true> : epilogue_back_kernel<true, false>)
+                          : (kept8 ? epilogue_back_kernel<false, true> : epilogue_back_kernel<false, false>);
+  kernel<<<grid, EB_THREADS, 0, st>>>(a);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || !a.dbias || a.plan.row_blocks == 1) return e;
   epilogue_bias_kernel<<<a.cols / 32 + (a.cols % 32 ? 1 : 0), 256, 0, st>>>(a.partial, a.plan.row_blocks, a.cols, a.accumulate, a.dbias);
   return hipGetLastError();

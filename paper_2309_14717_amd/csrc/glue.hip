@@ -4,6 +4,7 @@
 // elementwise launches in between.  bf16 in and out, fp32 arithmetic, 16-byte accesses.
 #include "common.hpp"
 #include "kernels.hpp"
+#include "swiglu.hpp"
 
 namespace qalora {
 
@@ -11,7 +12,6 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-__device__ __forceinline__ float sigmoidf_(float v) { return 1.0f / (1.0f + __expf(-v)); }
 }  // namespace
 
 // Element i of the flat index space is 16-byte piece i % c8 of row i / c8; gate, up (and their
@@ -28,14 +28,12 @@ __global__ __launch_bounds__(256) void swiglu_fwd_kernel(const u32x4* __restrict
     u32x4 o;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float g0 = lo_f(g[e]), g1 = hi_f(g[e]);
-      o[e] = pack_bf16x2(g0 * sigmoidf_(g0) * lo_f(u[e]), g1 * sigmoidf_(g1) * hi_f(u[e]));
+      o[e] = pack_bf16x2(swiglu_value(lo_f(g[e]), lo_f(u[e])), swiglu_value(hi_f(g[e]), hi_f(u[e])));
     }
     h[i] = o;
   }
 }
 
-// dgate = dh * up * d/dg[g sigmoid(g)] = dh * up * sig * (1 + g (1 - sig));  dup = dh * g * sig
 __global__ __launch_bounds__(256) void swiglu_bwd_kernel(const u32x4* __restrict__ dh,
                                                          const u32x4* __restrict__ gate,
                                                          const u32x4* __restrict__ up,
@@ -55,9 +53,7 @@ __global__ __launch_bounds__(256) void swiglu_bwd_kernel(const u32x4* __restrict
         const float dv = hsel ? hi_f(d[e]) : lo_f(d[e]);
         const float gv = hsel ? hi_f(g[e]) : lo_f(g[e]);
         const float uv = hsel ? hi_f(u[e]) : lo_f(u[e]);
-        const float sg = sigmoidf_(gv);
-        dg[hsel] = dv * uv * (sg * (1.0f + gv * (1.0f - sg)));
-        du[hsel] = dv * gv * sg;
+        swiglu_slopes(dv, gv, uv, dg[hsel], du[hsel]);
       }
       og[e] = pack_bf16x2(dg[0], dg[1]);
       ou[e] = pack_bf16x2(du[0], du[1]);

@@ -7,6 +7,7 @@
 #include "epilogue.hpp"
 #include "epilogue_plan.hpp"
 #include "grads_plan.hpp"
+#include "int8.hpp"
 #include "muon_plan.hpp"
 
 namespace qalora {
@@ -311,6 +312,7 @@ struct EpilogueBackArgs {
   const void* dy;       // [rows, cols] bf16 or fp32
   const uint16_t* z;    // bf16 [rows, cols]; null: not needed
   const uint16_t* mul;  // bf16 [rows, cols], or null
+  const uint8_t *z8, *mul8;  // or, instead of both: kept in 8 bits
   uint16_t* dz;         // bf16 [rows, cols], or null
   uint16_t* dmul;       // bf16 [rows, cols], or null
   float* dbias;         // [cols], or null
@@ -320,6 +322,60 @@ struct EpilogueBackArgs {
   EpilogueBackPlan plan;  // filled in by the launcher
 };
 hipError_t launch_epilogue_backward(const EpilogueBackArgs& a, hipStream_t st);
+
+// --- tokens8.hip: rows in 8 bits with one scale each ------------------------------------
+enum { TOKENS8_PLAIN = 0, TOKENS8_SCALED = 1, TOKENS8_SWIGLU = 2 };
+struct Tokens8Args {
+  const void* x;        // bf16 [rows, cols]; TOKENS8_SWIGLU: [rows, 2 cols], gate and up
+  const float* factor;  // TOKENS8_SCALED: [cols]
+  int8_t* codes;        // [rows, ld], zeros behind the columns
+  float* scale;         // [rows]
+  uint16_t* h;          // TOKENS8_SWIGLU: bf16 [rows, cols], or null
+  uint8_t* kept;        // TOKENS8_SWIGLU: keep8_bytes(2 rows, cols), or null
+  int rows, cols, ld, from;
+};
+hipError_t launch_tokens8(const Tokens8Args& a, hipStream_t st);
+struct Weight8Args {
+  const float* W;  // [d_in, d_out]; or, with bits, a quantized layer:
+  const uint32_t *plane0, *plane1;
+  const float *alpha, *beta;
+  int8_t* codes;  // [d_out, d_in]
+  float* scale;   // [d_out]
+  int d_in, d_out, group, bits;
+};
+hipError_t launch_weight8(const Weight8Args& a, hipStream_t st);
+
+// --- keep8.hip: activations kept in 8 bits ----------------------------------------------
+struct Keep8Args {
+  uint16_t* x;  // bf16 [rows, cols]: read by launch_keep8, written by launch_restore8
+  uint8_t* kept;
+  size_t rows;
+  int cols;
+};
+hipError_t launch_keep8(const Keep8Args& a, hipStream_t st);
+hipError_t launch_restore8(const Keep8Args& a, hipStream_t st);
+struct Swiglu8Args {
+  uint16_t* gu;  // bf16 [rows, 2 cols]: gate and up (read), or their gradients (written)
+  uint16_t* h;   // bf16 [rows, cols]: written, or its gradient (read)
+  uint8_t* kept;
+  size_t rows;
+  int cols;
+};
+hipError_t launch_swiglu_keep8(const Swiglu8Args& a, hipStream_t st);
+hipError_t launch_swiglu_kept8_backward(const Swiglu8Args& a, hipStream_t st);
+
+// --- gemm_i8.hip: products of 8-bit integers --------------------------------------------
+struct Int8GemmArgs {
+  const int8_t* tokens;    // [M, lda], zeros behind the K columns
+  const float* row_scale;  // [M]
+  const int8_t* codes;     // [d_out, d_in]: [N, K], or [K, N] with `back`
+  const float* col_scale;  // [N]; null with `back`
+  void* out;               // [M, N]
+  Epilogue epi;
+  int out_bf16, back;
+  int lda, M, N, K;
+};
+hipError_t launch_gemm_i8(const Int8GemmArgs& a, hipStream_t st);
 
 // --- muon.hip: the orthogonalised update of up to 32 matrices ------------------------------
 struct MuonHyper {

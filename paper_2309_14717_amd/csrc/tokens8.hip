@@ -1,0 +1,193 @@
+// Rows in 8 bits with one scale each: tokens (bf16, as they are, times a factor for each column, or as a SwiGLU's hidden activations)
+// and the channels of a weight.
+//   s = fl32(max |v| / 127),   code = rne(v / s)
+// The tokens' kernel reads a row once: a block (or a wavefront, for rows up to 1024 columns) has it whole in registers as bf16 when the
+// largest magnitude is known.  Bound by its bytes, 3 a column (SwiGLU: 5, and 2 more with the kept halves).
+#include "int8.hpp"
+#include "kernels.hpp"
+#include "swiglu.hpp"
+#include "tokens8_plan.hpp"
+
+namespace qalora {
+
+namespace {
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+}  // namespace
+
+template <int LANES, int PIECES, int FROM>
+__global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void tokens8_kernel(const Tokens8Args p) {
+  constexpr int WAVES = LANES / 64;
+  const int lane = threadIdx.x % LANES;
+  const size_t row = LANES == 64 ? (size_t)blockIdx.x * 4 + threadIdx.x / 64 : blockIdx.x;
+  if (LANES == 64 && row >= (size_t)p.rows) return;
+  const int eights = p.cols / 8;
+  auto value = [&](const u16x8& w, int at, int k) {
+    return FROM == TOKENS8_SCALED ? bf16_of(w, k) * p.factor[8 * at + k] : bf16_of(w, k);
+  };
+
+  u16x8 held[PIECES];
+  uint32_t top = 0;
+#pragma unroll
+  for (int q = 0; q < PIECES; ++q) {
+    const int at = lane + q * LANES;
+    held[q] = u16x8{0, 0, 0, 0};
+    if (FROM == TOKENS8_SWIGLU) {
+      u16x8 g{0, 0, 0, 0}, u{0, 0, 0, 0};
+      if (at < eights) {
+        const u16x8* src = reinterpret_cast<const u16x8*>(p.x) + row * 2 * eights + at;
+        g = src[0];
+        u = src[eights];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        held[q][k] = pack_bf16x2(swiglu_value(bf16_of(g, 2 * k), bf16_of(u, 2 * k)),
+                                 swiglu_value(bf16_of(g, 2 * k + 1), bf16_of(u, 2 * k + 1)));
+      if (p.kept) {  // (a group's four lanes go together: lanes past the row have zeros)
+        const uint32_t eg = group_exponent(g), eu = group_exponent(u);
+        if (at < eights) {
+          u8x8* codes = reinterpret_cast<u8x8*>(p.kept) + row * 2 * eights + at;
+          codes[0] = group_codes(g, eg);
+          codes[eights] = group_codes(u, eu);
+          if (at % 4 == 0) {
+            const size_t groups = keep8_groups(p.cols);
+            uint8_t* e = p.kept + keep8_exponents_at(2 * (size_t)p.rows, p.cols) + row * 2 * groups + at / 4;
+            e[0] = (uint8_t)eg;
+            e[groups] = (uint8_t)eu;
+          }
+        }
+      }
+      if (p.h && at < eights) reinterpret_cast<u16x8*>(p.h)[row * eights + at] = held[q];
+    } else if (at < eights) {
+      held[q] = reinterpret_cast<const u16x8*>(p.x)[row * eights + at];
+    }
+    if (at < eights)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) top = max(top, magnitude(value(held[q], at, k)));
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+  if constexpr (WAVES > 1) {
+    __shared__ uint32_t tops[WAVES];
+    if (threadIdx.x % 64 == 0) tops[threadIdx.x / 64] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) top = max(top, tops[w]);
+  }
+  const RowScale r = row_scale_of(top);
+  if (lane == 0) p.scale[row] = r.s;
+#pragma unroll
+  for (int q = 0; q < PIECES; ++q) {
+    const int at = lane + q * LANES;
+    if (at < p.ld / 8) {  // (the columns up to a longer row's end are zeros)
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = at < eights ? value(held[q], at, k) : 0.0f;
+      reinterpret_cast<u8x8*>(p.codes)[row * (p.ld / 8) + at] = row_codes(v, r);
+    }
+  }
+}
+
+hipError_t launch_tokens8(const Tokens8Args& a, hipStream_t st) {
+  const Tokens8Plan plan = tokens8_plan(a.ld);
+  auto go = [&](auto from_c) {
+    constexpr int FROM = decltype(from_c)::value;
+    const unsigned blocks = (unsigned)(((size_t)a.rows + plan.rows - 1) / plan.rows);
+    switch (plan.lanes * 100 + plan.pieces) {
+      case 6401: tokens8_kernel<64, 1, FROM><<<blocks, 256, 0, st>>>(a); break;
+      case 6402: tokens8_kernel<64, 2, FROM><<<blocks, 256, 0, st>>>(a); break;
+      case 25601: tokens8_kernel<256, 1, FROM><<<blocks, 256, 0, st>>>(a); break;
+      case 25602: tokens8_kernel<256, 2, FROM><<<blocks, 256, 0, st>>>(a); break;
+      case 25604: tokens8_kernel<256, 4, FROM><<<blocks, 256, 0, st>>>(a); break;
+      case 102402: tokens8_kernel<1024, 2, FROM><<<blocks, 1024, 0, st>>>(a); break;
+      case 102404: tokens8_kernel<1024, 4, FROM><<<blocks, 1024, 0, st>>>(a); break;
+      case 102408: tokens8_kernel<1024, 8, FROM><<<blocks, 1024, 0, st>>>(a); break;
+      case 102416: tokens8_kernel<1024, 16, FROM><<<blocks, 1024, 0, st>>>(a); break;
+      default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+  };
+  switch (a.from) {
+    case TOKENS8_PLAIN: return go(std::integral_constant<int, TOKENS8_PLAIN>{});
+    case TOKENS8_SCALED: return go(std::integral_constant<int, TOKENS8_SCALED>{});
+    default: return go(std::integral_constant<int, TOKENS8_SWIGLU>{});
+  }
+}
+
+// ---- a weight's channels -------------------------------------------------------------------------------------------------
+// W [d_in, d_out] fp32, or alpha code + beta (one rounding) of a quantized layer, to codes [d_out, d_in].  Done once for a model: the
+// channels' largest magnitudes (by atomic maxima of their bits, whose order does not matter), then the codes, then the scales.
+
+template <int NBITS>  // 0: W
+__device__ __forceinline__ float weight_at(const Weight8Args& p, int i, int j) {
+  if constexpr (NBITS == 0) {
+    return p.W[(size_t)i * p.d_out + j];
+  } else {
+    constexpr int RB = PackFmt<NBITS>::kRowsPerWord0, LB = NBITS == 3 ? 2 : NBITS;
+    const int r = i % RB;
+    uint32_t code = (p.plane0[(size_t)(i / RB) * p.d_out + j] >> (LB * (r >> 1) + 16 * (r & 1))) & ((1u << LB) - 1);
+    if constexpr (NBITS == 3) {
+      const int r1 = i % 32;
+      code |= ((p.plane1[(size_t)(i / 32) * p.d_out + j] >> ((r1 >> 1) + 16 * (r1 & 1))) & 1u) << 2;
+    }
+    const size_t at = (size_t)(i / p.group) * p.d_out + j;
+    return __builtin_fmaf(p.alpha[at], (float)code, p.beta[at]);
+  }
+}
+
+__global__ __launch_bounds__(256) void weight8_clear_kernel(const Weight8Args p) {
+  const int j = blockIdx.x * 256 + threadIdx.x;
+  if (j < p.d_out) p.scale[j] = 0.0f;
+}
+constexpr int W8_ROWS = 256;  // of W, a block's share of a channel's magnitudes
+template <int NBITS>
+__global__ __launch_bounds__(256) void weight8_top_kernel(const Weight8Args p) {
+  const int j = blockIdx.x * 256 + threadIdx.x;
+  if (j >= p.d_out) return;
+  const int i0 = blockIdx.y * W8_ROWS, i1 = min(p.d_in, i0 + W8_ROWS);
+  uint32_t top = 0;
+#pragma unroll 8
+  for (int i = i0; i < i1; ++i) top = max(top, magnitude(weight_at<NBITS>(p, i, j)));
+  atomicMax(reinterpret_cast<uint32_t*>(p.scale) + j, top);
+}
+// 64 rows of W by 64 channels, transposed through LDS
+template <int NBITS>
+__global__ __launch_bounds__(256) void weight8_codes_kernel(const Weight8Args p) {
+  __shared__ uint8_t tile[64][64 + 4];
+  const int c = threadIdx.x % 64, j = blockIdx.x * 64 + c, i0 = blockIdx.y * 64;
+  if (j < p.d_out) {
+    const RowScale r = row_scale_of(reinterpret_cast<const uint32_t*>(p.scale)[j]);
+    for (int k = threadIdx.x / 64; k < 64 && i0 + k < p.d_in; k += 4)
+      tile[c][k] = r.inv > 0.0f ? (uint8_t)__float_as_uint(row_code(weight_at<NBITS>(p, i0 + k, j), r)) : (uint8_t)0;
+  }
+  __syncthreads();
+  const int t = threadIdx.x / 16, q = threadIdx.x % 16;  // sixteen lanes a channel, four rows each
+  if (i0 + 4 * q >= p.d_in) return;                      // (d_in is a multiple of 16)
+  for (int k = t; k < 64; k += 16)
+    if (blockIdx.x * 64 + k < (unsigned)p.d_out)
+      *reinterpret_cast<uint32_t*>(p.codes + (size_t)(blockIdx.x * 64 + k) * p.d_in + i0 + 4 * q) =
+          *reinterpret_cast<const uint32_t*>(&tile[k][4 * q]);
+}
+__global__ __launch_bounds__(256) void weight8_scale_kernel(const Weight8Args p) {
+  const int j = blockIdx.x * 256 + threadIdx.x;
+  if (j < p.d_out) p.scale[j] = row_scale_of(reinterpret_cast<const uint32_t*>(p.scale)[j]).s;
+}
+
+hipError_t launch_weight8(const Weight8Args& a, hipStream_t st) {
+  const unsigned by256 = ceil_div(a.d_out, 256);
+  auto go = [&](auto bits_c) {
+    constexpr int NBITS = decltype(bits_c)::value;
+    weight8_clear_kernel<<<by256, 256, 0, st>>>(a);
+    weight8_top_kernel<NBITS><<<dim3(by256, ceil_div(a.d_in, W8_ROWS)), 256, 0, st>>>(a);
+    weight8_codes_kernel<NBITS><<<dim3(ceil_div(a.d_out, 64), ceil_div(a.d_in, 64)), 256, 0, st>>>(a);
+    weight8_scale_kernel<<<by256, 256, 0, st>>>(a);
+    return hipGetLastError();
+  };
+  switch (a.bits) {
+    case 0: return go(std::integral_constant<int, 0>{});
+    case 2: return go(std::integral_constant<int, 2>{});
+    case 3: return go(std::integral_constant<int, 3>{});
+    default: return go(std::integral_constant<int, 4>{});
+  }
+}
+
+}  // namespace qalora
