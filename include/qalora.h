@@ -298,7 +298,8 @@ int qalora_epilogue_backward(int act, int tokens, int cols, const void* dy, int 
  *             forward with the codes of x taken for x, and with dy's own rounding to 8 bits per token (at most s / 2 an element of v).
  *             The weight is frozen; the bias's gradient is qalora_epilogue_backward's.
  * codes int8 [d_out, d_in], scale fp32 [d_out]: one copy serves both directions.  d_in a multiple of 16, d_out a multiple of 8, both at
- * most QALORA_INT8_MAX_SIDE (the sums then fit 32 bits); QALORA_EUNSUPPORTED otherwise.  No other limit on sizes: operands may pass 4 GB.
+ * most QALORA_INT8_MAX_SIDE (the sums then fit 32 bits), tokens of a product at most 2^29;
+ * QALORA_EUNSUPPORTED otherwise.  Operands may pass 4 GB.
  * All of these may be captured into a HIP graph after one eager call of the same shape; reruns are bit-identical. */
 #define QALORA_INT8_MAX_SIDE 131072
 /* W fp32 [d_in, d_out] (row-major, as everywhere) -> codes [d_out, d_in], scale [d_out]. */

@@ -19,7 +19,8 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libqalora_hip.so")
 SOURCES = ["api.hip", "quantize.hip", "gemm_dq.hip", "adapter.hip", "smallt.hip", "smallt4.hip", "smallt4_f16.hip",
            "midt.hip", "glue.hip", "optim.hip", "probe.hip", "compensate.hip", "gemm_dq_192.hip",
-           "grads.hip", "muon.hip", "epilogue.hip", "gemm_dq_epi.hip", "tokens8.hip", "keep8.hip", "gemm_i8.hip"]
+           "grads.hip", "muon.hip", "epilogue.hip", "gemm_dq_epi.hip", "tokens8.hip", "keep8.hip", "gemm_i8.hip",
+           "stream_i8.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 LLVM = os.environ.get("HIP_CLANG_PATH", "/opt/rocm/llvm/bin")
 FLAGS = [
@@ -38,7 +39,7 @@ FLAGS = [
 NO_SCRATCH = {"gemm_dq.hip": "gemm_dq_kernel", "gemm_dq_192.hip": "gemm_dq_kernel", "gemm_dq_epi.hip": "gemm_dq_kernel", "midt.hip": "midt_kernel", "smallt.hip": "smallt_kernel", "smallt4.hip": "smallt4_kernel", "smallt4_f16.hip": "smallt4_kernel",
               "adapter.hip": ("front_kernel", "front_wide_kernel"), "grads.hip": ("z_kernel", "finish_kernel", "fused_kernel", "du_kernel", "db_kernel", "tail_kernel"),
               "muon.hip": ("muon_start_kernel", "muon_pass_kernel", "muon_alone_kernel"), "epilogue.hip": "epilogue_back_kernel",
-              "tokens8.hip": "tokens8_kernel", "gemm_i8.hip": "gemm_i8_kernel"}
+              "tokens8.hip": "tokens8_kernel", "gemm_i8.hip": "gemm_i8_kernel", "stream_i8.hip": "stream_i8_kernel"}
 
 
 def _as_tuple(v):

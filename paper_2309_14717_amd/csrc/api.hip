@@ -3,9 +3,11 @@
 #include "../../include/qalora.h"
 
 #include "common.hpp"
+#include "gemm_i8_plan.hpp"
 #include "gemm_plan.hpp"
 #include "kernels.hpp"
 #include "midt_plan.hpp"
+#include "stream_i8_plan.hpp"
 #include "tokens8_plan.hpp"
 
 #include <algorithm>
@@ -843,23 +845,24 @@ int qalora_quantize_tokens(int tokens, int cols, const void* x, const float* fac
   return launch_tokens8(a, as_stream(stream)) == hipSuccess ? QALORA_OK : QALORA_EHIP;
 }
 
-// Workspace of the products: the codes and scales of the tokens (rows of whole 16 bytes).
-struct Int8Plan {
-  size_t q, s, total;
+// Workspace of the products: the codes and scales of the tokens (rows of whole 16 bytes), and the sums of slices of K.
+struct Int8Room {
+  size_t q, s, partial, total;
   int ld;
 };
-static Int8Plan plan_int8(int tokens, int K) {
-  Int8Plan p{};
+static Int8Room int8_room(int tokens, int N, int K) {
+  Int8Room p{};
   Carver c;
   p.ld = round_up(K, 16);
   p.s = c.take(sizeof(float) * (size_t)tokens);
   p.q = c.take((size_t)tokens * p.ld);
+  p.partial = c.take(int8_partials(tokens, N));
   p.total = c.off;
   return p;
 }
 size_t qalora_int8_workspace_bytes(int tokens, int d_in, int d_out, int op) {
-  if (tokens <= 0 || int8_sizes(d_in, d_out) != QALORA_OK || (op != QALORA_OP_FORWARD && op != QALORA_OP_BACKWARD)) return 0;
-  return plan_int8(tokens, op == QALORA_OP_FORWARD ? d_in : d_out).total;
+  if (tokens <= 0 || tokens > I8_MAX_TOKENS || int8_sizes(d_in, d_out) != QALORA_OK || (op != QALORA_OP_FORWARD && op != QALORA_OP_BACKWARD)) return 0;
+  return op == QALORA_OP_FORWARD ? int8_room(tokens, d_out, d_in).total : int8_room(tokens, d_in, d_out).total;
 }
 
 int qalora_forward_int8(int tokens, int d_in, int d_out, const void* x, const float* x_scale, const int8_t* codes,
@@ -868,12 +871,13 @@ int qalora_forward_int8(int tokens, int d_in, int d_out, const void* x, const fl
   if (tokens <= 0 || !x || !codes || !scale || !y) return QALORA_EINVAL;
   if (y_dtype != QALORA_F32 && y_dtype != QALORA_BF16) return QALORA_EINVAL;
   if (const int rc = int8_sizes(d_in, d_out); rc != QALORA_OK) return rc;
+  if (tokens > I8_MAX_TOKENS) return QALORA_EUNSUPPORTED;
   Epilogue e{};
   const Epilogue* use;
   if (const int rc = read_epilogue(epilogue, y, e, &use); rc != QALORA_OK) return rc;
   if (misaligned(x) || misaligned(x_scale) || misaligned(codes) || misaligned(scale) || misaligned(y) || misaligned(ws))
     return QALORA_EALIGN;
-  const Int8Plan plan = plan_int8(tokens, d_in);
+  const Int8Room plan = int8_room(tokens, d_out, d_in);
   if (!ws || ws_bytes < plan.total) return QALORA_EWORKSPACE;
   const size_t n = (size_t)tokens * d_out;
   const Span weights{codes, (size_t)d_in * d_out}, scales{scale, sizeof(float) * d_out},
@@ -882,6 +886,19 @@ int qalora_forward_int8(int tokens, int d_in, int d_out, const void* x, const fl
       any_overlap({y, n * (y_dtype == QALORA_BF16 ? 2 : 4)}, {weights, scales, x_scales}) ||
       any_overlap({e.z, 2 * n}, {weights, scales, x_scales}))
     return QALORA_EINVAL;
+  if (!x_scale && stream8_takes(tokens, d_in)) {
+    StreamI8Args a{};
+    a.x = static_cast<const uint16_t*>(x);
+    a.codes = codes;
+    a.col_scale = scale;
+    a.out = y;
+    a.out_bf16 = y_dtype == QALORA_BF16;
+    a.epi = e;
+    a.M = tokens;
+    a.N = d_out;
+    a.K = d_in;
+    return launch_stream_i8(a, as_stream(stream)) == hipSuccess ? QALORA_OK : QALORA_EHIP;
+  }
   char* w = static_cast<char*>(ws);
   Int8GemmArgs g{};
   if (x_scale) {
@@ -904,6 +921,7 @@ int qalora_forward_int8(int tokens, int d_in, int d_out, const void* x, const fl
   }
   g.codes = codes;
   g.col_scale = scale;
+  g.partial = reinterpret_cast<int*>(w + plan.partial);
   g.out = y;
   g.out_bf16 = y_dtype == QALORA_BF16;
   g.epi = e;
@@ -918,9 +936,10 @@ int qalora_backward_int8(int tokens, int d_in, int d_out, const void* dy, const 
   if (tokens <= 0 || !dy || !codes || !scale || !dx) return QALORA_EINVAL;
   if (dx_dtype != QALORA_F32 && dx_dtype != QALORA_BF16) return QALORA_EINVAL;
   if (const int rc = int8_sizes(d_in, d_out); rc != QALORA_OK) return rc;
+  if (tokens > I8_MAX_TOKENS) return QALORA_EUNSUPPORTED;
   if (misaligned(dy) || misaligned(codes) || misaligned(scale) || misaligned(residual) || misaligned(dx) || misaligned(ws))
     return QALORA_EALIGN;
-  const Int8Plan plan = plan_int8(tokens, d_out);
+  const Int8Room plan = int8_room(tokens, d_in, d_out);
   if (!ws || ws_bytes < plan.total) return QALORA_EWORKSPACE;
   const Span out{dx, (size_t)tokens * d_in * (dx_dtype == QALORA_BF16 ? 2 : 4)};
   if (any_overlap(out, {{dy, 2 * (size_t)tokens * d_out}, {codes, (size_t)d_in * d_out}, {scale, sizeof(float) * d_out}}) ||
@@ -942,6 +961,7 @@ int qalora_backward_int8(int tokens, int d_in, int d_out, const void* dy, const 
   g.row_scale = a.scale;
   g.lda = plan.ld;
   g.codes = codes;
+  g.partial = reinterpret_cast<int*>(w + plan.partial);
   g.out = dx;
   g.out_bf16 = dx_dtype == QALORA_BF16;
   g.epi.residual = residual;

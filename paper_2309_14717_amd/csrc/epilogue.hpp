@@ -136,4 +136,28 @@ __device__ __forceinline__ f32x4 apply_epilogue(const Epilogue& e, f32x4 v, size
   return v;
 }
 
+// The operands of four neighbouring elements, requested before the sums are there, and y of them.
+struct EpilogueFour {
+  f32x4 bias, mul, residual;
+};
+__device__ __forceinline__ void request_four(const Epilogue& e, size_t at, int col, int out_bf16, EpilogueFour& o) {
+  typedef uint32_t pair __attribute__((ext_vector_type(2)));
+  if (e.bias) o.bias = *reinterpret_cast<const f32x4*>(e.bias + col);
+  auto halves = [](const pair& w) {
+    return f32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u), __uint_as_float(w[1] << 16), __uint_as_float(w[1] & 0xffff0000u)};
+  };
+  if (e.mul) o.mul = halves(*reinterpret_cast<const pair*>(e.mul + at));
+  if (e.residual && out_bf16) o.residual = halves(*reinterpret_cast<const pair*>(static_cast<const uint16_t*>(e.residual) + at));
+  else if (e.residual) o.residual = *reinterpret_cast<const f32x4*>(static_cast<const float*>(e.residual) + at);
+}
+__device__ __forceinline__ f32x4 apply_four(const Epilogue& e, const EpilogueFour& o, f32x4 v, size_t at) {
+  typedef uint32_t pair __attribute__((ext_vector_type(2)));
+  if (e.bias) v += o.bias;
+  if (e.z) *reinterpret_cast<pair*>(e.z + at) = pair{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+  act_values<4>(e.act, v);
+  if (e.mul) v *= o.mul;
+  if (e.residual) v += o.residual;
+  return v;
+}
+
 }  // namespace qalora

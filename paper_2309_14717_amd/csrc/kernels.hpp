@@ -333,6 +333,7 @@ struct Tokens8Args {
   uint16_t* h;          // TOKENS8_SWIGLU: bf16 [rows, cols], or null
   uint8_t* kept;        // TOKENS8_SWIGLU: keep8_bytes(2 rows, cols), or null
   int rows, cols, ld, from;
+  int row_begin, row_end;  // filled in by the launcher
 };
 hipError_t launch_tokens8(const Tokens8Args& a, hipStream_t st);
 struct Weight8Args {
@@ -371,11 +372,23 @@ struct Int8GemmArgs {
   const int8_t* codes;     // [d_out, d_in]: [N, K], or [K, N] with `back`
   const float* col_scale;  // [N]; null with `back`
   void* out;               // [M, N]
+  int* partial;            // int8_partials(M, N)
   Epilogue epi;
   int out_bf16, back;
   int lda, M, N, K;
 };
 hipError_t launch_gemm_i8(const Int8GemmArgs& a, hipStream_t st);
+
+// --- stream_i8.hip: the same, forward, for few tokens that come in bf16 -----------------
+struct StreamI8Args {
+  const uint16_t* x;       // bf16 [M, K]
+  const int8_t* codes;     // [N, K]
+  const float* col_scale;  // [N]
+  void* out;               // [M, N]
+  Epilogue epi;
+  int out_bf16, M, N, K;
+};
+hipError_t launch_stream_i8(const StreamI8Args& a, hipStream_t st);
 
 // --- muon.hip: the orthogonalised update of up to 32 matrices ------------------------------
 struct MuonHyper {

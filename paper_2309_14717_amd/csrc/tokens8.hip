@@ -18,11 +18,17 @@ template <int LANES, int PIECES, int FROM>
 __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void tokens8_kernel(const Tokens8Args p) {
   constexpr int WAVES = LANES / 64;
   const int lane = threadIdx.x % LANES;
-  const size_t row = LANES == 64 ? (size_t)blockIdx.x * 4 + threadIdx.x / 64 : blockIdx.x;
-  if (LANES == 64 && row >= (size_t)p.rows) return;
+  const size_t row = (size_t)p.row_begin + (LANES == 64 ? blockIdx.x * 4 + threadIdx.x / 64 : blockIdx.x);
+  if (LANES == 64 && row >= (size_t)p.row_end) return;
   const int eights = p.cols / 8;
-  auto value = [&](const u16x8& w, int at, int k) {
-    return FROM == TOKENS8_SCALED ? bf16_of(w, k) * p.factor[8 * at + k] : bf16_of(w, k);
+  auto values = [&](const u16x8& w, int at, float (&v)[8]) {
+    f32x4 f[2];
+    if (FROM == TOKENS8_SCALED) {
+      f[0] = reinterpret_cast<const f32x4*>(p.factor)[2 * at];
+      f[1] = reinterpret_cast<const f32x4*>(p.factor)[2 * at + 1];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = FROM == TOKENS8_SCALED ? bf16_of(w, k) * f[k >> 2][k & 3] : bf16_of(w, k);
   };
 
   u16x8 held[PIECES];
@@ -60,9 +66,12 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void tokens8_kernel(cons
     } else if (at < eights) {
       held[q] = reinterpret_cast<const u16x8*>(p.x)[row * eights + at];
     }
-    if (at < eights)
+    if (at < eights) {
+      float v[8];
+      values(held[q], at, v);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) top = max(top, magnitude(value(held[q], at, k)));
+      for (int k = 0; k < 8; ++k) top = max(top, magnitude(v[k]));
+    }
   }
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
@@ -79,19 +88,19 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void tokens8_kernel(cons
   for (int q = 0; q < PIECES; ++q) {
     const int at = lane + q * LANES;
     if (at < p.ld / 8) {  // (the columns up to a longer row's end are zeros)
-      float v[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = at < eights ? value(held[q], at, k) : 0.0f;
+      float v[8] = {};
+      if (at < eights) values(held[q], at, v);
       reinterpret_cast<u8x8*>(p.codes)[row * (p.ld / 8) + at] = row_codes(v, r);
     }
   }
 }
 
-hipError_t launch_tokens8(const Tokens8Args& a, hipStream_t st) {
-  const Tokens8Plan plan = tokens8_plan(a.ld);
+hipError_t launch_tokens8(const Tokens8Args& args, hipStream_t st) {
+  const Tokens8Plan plan = tokens8_plan(args.ld);
+  Tokens8Args a = args;
   auto go = [&](auto from_c) {
     constexpr int FROM = decltype(from_c)::value;
-    const unsigned blocks = (unsigned)(((size_t)a.rows + plan.rows - 1) / plan.rows);
+    const unsigned blocks = (unsigned)((a.row_end - a.row_begin + plan.rows - 1) / plan.rows);
     switch (plan.lanes * 100 + plan.pieces) {
       case 6401: tokens8_kernel<64, 1, FROM><<<blocks, 256, 0, st>>>(a); break;
       case 6402: tokens8_kernel<64, 2, FROM><<<blocks, 256, 0, st>>>(a); break;
@@ -106,11 +115,17 @@ hipError_t launch_tokens8(const Tokens8Args& a, hipStream_t st) {
     }
     return hipGetLastError();
   };
-  switch (a.from) {
-    case TOKENS8_PLAIN: return go(std::integral_constant<int, TOKENS8_PLAIN>{});
-    case TOKENS8_SCALED: return go(std::integral_constant<int, TOKENS8_SCALED>{});
-    default: return go(std::integral_constant<int, TOKENS8_SWIGLU>{});
+  hipError_t e = hipSuccess;
+  for (int r = 0; r < a.rows && e == hipSuccess; r = a.row_end) {  // (a launch has at most 2^32 threads)
+    a.row_begin = r;
+    a.row_end = a.rows - r > T8_MOST_ROWS ? r + T8_MOST_ROWS : a.rows;
+    switch (a.from) {
+      case TOKENS8_PLAIN: e = go(std::integral_constant<int, TOKENS8_PLAIN>{}); break;
+      case TOKENS8_SCALED: e = go(std::integral_constant<int, TOKENS8_SCALED>{}); break;
+      default: e = go(std::integral_constant<int, TOKENS8_SWIGLU>{}); break;
+    }
   }
+  return e;
 }
 
 // ---- a weight's channels -------------------------------------------------------------------------------------------------

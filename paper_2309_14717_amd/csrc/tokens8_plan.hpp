@@ -5,7 +5,7 @@
 namespace qalora {
 
 constexpr int T8_MAX_COLS = 1 << 17;  // 1024 threads with sixteen pieces of eight columns each
-constexpr int T8_MAX_PIECES = 16;
+constexpr int T8_MOST_ROWS = 1 << 21;  // of a launch
 
 struct Tokens8Plan {
   int lanes;   // threads along a row: 64, 256 or 1024

@@ -4,6 +4,15 @@ import torch
 
 BF16, F32 = torch.bfloat16, torch.float32
 
+# tokens, d_in, d_out: one token to long batches, widths that end inside every tile, every tile and K split (a test without a GPU
+# looks at that)
+SHAPES = [(1, 16, 8), (1, 4096, 1032), (3, 1024, 264), (4, 11008, 520), (7, 48, 24), (16, 1024, 1024), (16, 272, 136), (17, 5120, 520),
+          (31, 144, 72), (33, 4096, 264), (61, 1040, 776), (64, 1024, 1024), (65, 256, 72), (100, 2064, 520), (128, 512, 512),
+          (129, 4112, 1544), (200, 208, 2056), (257, 1024, 328), (511, 96, 40), (700, 1536, 1288), (1031, 784, 600)]
+BACK_SHAPES = [(5, 64, 11008), (300, 16, 4104)]
+# tokens, depth and width of the product, for the larger tiles
+LARGE = [(700, 64, 16400), (500, 144, 16400), (380, 64, 11024), (380, 272, 8208), (250, 144, 4112), (140, 272, 16400), (513, 80, 8208)]
+
 
 def rows8(v):
     """Codes (float64) and scales (float32) of the rows of v, an fp32 tensor on the CPU.  The quotient of two fp32 numbers differs from

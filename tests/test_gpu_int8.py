@@ -5,15 +5,9 @@ import torch
 
 import epilogue_cases as ec
 import int8_cases as ic
-from int8_cases import BF16, F32, same
+from int8_cases import BACK_SHAPES, BF16, F32, SHAPES, same
 
 pytestmark = pytest.mark.gpu
-
-# tokens, d_in, d_out: one token to long batches, widths that end inside every tile
-SHAPES = [(1, 16, 8), (1, 4096, 1032), (3, 1024, 264), (4, 11008, 520), (7, 48, 24), (16, 1024, 1024), (16, 272, 136), (17, 5120, 520),
-          (31, 144, 72), (33, 4096, 264), (61, 1040, 776), (64, 1024, 1024), (65, 256, 72), (100, 2064, 520), (128, 512, 512),
-          (129, 4112, 1544), (200, 208, 2056), (257, 1024, 328), (511, 96, 40), (700, 1536, 1288), (1031, 784, 600)]
-
 
 @pytest.mark.parametrize("cols", [8, 24, 264, 1000, 1024, 1032, 2048, 4096, 5000, 8192, 8200, 11008, 22016, 32768, 40000, 65536, 131072])
 @pytest.mark.parametrize("scaled", [False, True])
@@ -138,7 +132,7 @@ def test_forward(gpu_api, shape):
         same(stream, gpu_api.forward_int8(tokens8, *w, residual=residual.cuda(), out_dtype=out_dtype))
 
 
-@pytest.mark.parametrize("shape", SHAPES + [(5, 64, 11008), (300, 16, 4104)], ids=str)
+@pytest.mark.parametrize("shape", SHAPES + BACK_SHAPES, ids=str)
 def test_backward(gpu_api, shape):
     T, d_in, d_out = shape
     codes, scale = ic.drawn_weight(3, d_in, d_out)
@@ -181,6 +175,35 @@ def test_gradient_is_the_forwards_difference(gpu_api, shape):
     y = lambda v: gpu_api.forward_int8(v.to(BF16).cuda(), codes, scale).double().cpu()  # noqa: E731
     dx = gpu_api.backward_int8(dy.to(BF16).cuda(), codes, scale).double().cpu()
     assert float((dy.double() * (y(x + d) - y(x - d))).sum()) == 2 * float((dx * d.double()).sum())
+
+
+@pytest.mark.parametrize("size", ic.LARGE, ids=str)
+def test_large_tiles(gpu_api, size):
+    """Both directions of a product, with an epilogue, against 64 bits on the GPU."""
+    T, depth, width = size
+    codes, scale = (t.cuda() for t in ic.drawn_weight(7, depth, width))
+    q, s = gpu_api.quantize_tokens(ic.drawn_tokens(8, T, depth).cuda())
+    acc = q.double() @ codes.double().T
+    ref = acc.to(F32) * s[:, None] * scale
+    same(gpu_api.forward_int8((q, s), codes, scale), ref)
+    bias, mul, residual = (t.cuda() for t in ec.extras(3, T, width, BF16))
+    y, z = gpu_api.forward_int8((q, s), codes, scale, bias=bias, act="silu", mul=mul, residual=residual, keep_z=True, out_dtype=BF16)
+    z64 = (acc.to(F32) * s[:, None]).double() * scale.double() + bias.double()
+    off = 2.0 ** -24 * (ref.double().abs() + z64.abs())
+    assert ((z.double() - z64).abs() <= off + 2.0 ** -8 * (z64.abs() + off)).all()
+    y64, tol = ec.after(z64, "silu", mul, residual)
+    tol = tol + 1.2 * off * mul.double().abs()
+    assert ((y.double() - y64).abs() <= tol + 2.0 ** -8 * (y64.abs() + tol)).all()
+    dy = ic.drawn_tokens(9, T, depth).cuda()                    # [tokens, d_out], d_out = depth here
+    w, ws = codes.T.contiguous(), torch.rand(depth, device="cuda") + 0.5
+    q, s = gpu_api.quantize_tokens(dy, ws)
+    acc = q.double() @ w.double()
+    same(gpu_api.backward_int8(dy, w, ws), acc.to(F32) * s[:, None])
+    r = torch.randn((T, width), device="cuda").to(BF16)
+    ref64 = acc * s[:, None].double() + r.double()
+    tol = 2.0 ** -24 * (2 * (acc * s[:, None].double()).abs() + ref64.abs())
+    got = gpu_api.backward_int8(dy, w, ws, residual=r, dx_dtype=BF16)
+    assert ((got.double() - ref64).abs() <= tol + 2.0 ** -8 * (ref64.abs() + tol)).all()
 
 
 def test_largest_sums(gpu_api):

@@ -1,5 +1,6 @@
 """The 8-bit operators without a GPU: their refusals, sizes and launch shapes, and the gradients' formulas against differences."""
 import ctypes
+import random
 
 import pytest
 import torch
@@ -9,6 +10,7 @@ from host_code import host_library
 from paper_2309_14717_amd import api
 
 SOURCE = r"""
+#include "gemm_i8_plan.hpp"
 #include "int8.hpp"
 #include "tokens8_plan.hpp"
 using namespace qalora;
@@ -16,6 +18,11 @@ extern "C" void tokens(int cols, int* o) {
   const Tokens8Plan p = tokens8_plan(cols);
   o[0] = p.lanes; o[1] = p.pieces; o[2] = p.rows;
 }
+extern "C" void product(int M, int N, int K, int back, int* o) {
+  const Int8Plan p = int8_plan(M, N, K, back);
+  o[0] = p.tile; o[1] = p.slices; o[2] = kInt8Tiles[p.tile].rows; o[3] = kInt8Tiles[p.tile].cols; o[4] = kInt8Tiles[p.tile].threads;
+}
+extern "C" long long partials(int M, int N) { return (long long)int8_partials(M, N); }
 extern "C" long long kept(long long rows, long long cols) { return (long long)keep8_bytes(rows, cols); }
 extern "C" long long exponents_at(long long rows, long long cols) { return (long long)keep8_exponents_at(rows, cols); }
 """
@@ -26,7 +33,7 @@ GOOD, ODD = 0x10000, 0x10004
 @pytest.fixture(scope="module")
 def host(tmp_path_factory):
     lib = host_library(tmp_path_factory.mktemp("int8"), "int8_plan", SOURCE)
-    lib.kept.restype = lib.exponents_at.restype = ctypes.c_longlong
+    lib.kept.restype = lib.exponents_at.restype = lib.partials.restype = ctypes.c_longlong
     lib.kept.argtypes = lib.exponents_at.argtypes = [ctypes.c_longlong] * 2
     return lib
 
@@ -39,6 +46,33 @@ def test_rows_are_covered(host):
         assert lanes * pieces * 8 >= cols and (lanes, pieces) in {(64, 1), (64, 2), (256, 1), (256, 2), (256, 4), (1024, 2), (1024, 4),
                                                                   (1024, 8), (1024, 16)}
         assert rows == (4 if lanes == 64 else 1)
+
+
+def test_product_plans(host):
+    """Slices that are all there and fit their room, launches that the device takes; and the GPU tests reach every tile and a split."""
+    o = (ctypes.c_int * 5)()
+    rng = random.Random(3)
+    sizes = [(1, 8, 16), (2 ** 29, 8, 16), (2 ** 29, 256, 16), (2 ** 27, 1032, 16), (1, 131072, 131072), (4096, 11008, 4096), (1, 8, 131072)]
+    sizes += [(rng.randint(1, 10 ** rng.randint(1, 6)), 8 * rng.randint(1, 4000), 16 * rng.randint(1, 2000)) for _ in range(2000)]
+    for M, N, K in sizes:
+        for back in (0, 1):
+            host.product(M, N, K, back, o)
+            _, slices, rows, cols, threads = o
+            steps = -(-K // 128)
+            per = -(-steps // slices)
+            assert per * (slices - 1) < steps <= per * slices and slices <= 32
+            assert slices == 1 or slices * M * N * 4 <= host.partials(M, N)
+            assert -(-M // rows) * -(-N // cols) * threads < 2 ** 32
+    for shapes, back in ((ic.SHAPES, 0), (ic.SHAPES + ic.BACK_SHAPES, 1)):
+        got = set()
+        for T, d_in, d_out in shapes:
+            host.product(T, d_in if back else d_out, d_out if back else d_in, back, o)
+            got.add((o[0], o[1] > 1))
+        assert {s for _, s in got} == {False, True}
+        for T, depth, width in ic.LARGE:
+            host.product(T, width, depth, back, o)
+            got.add((o[0], o[1] > 1))
+        assert {t for t, _ in got} == set(range(11)) - ({4, 6, 8, 10} if back else {7, 9}), (back, sorted(got))
 
 
 def test_kept_sizes(host):
@@ -74,7 +108,7 @@ def test_argument_errors_are_caught_before_launch():
                 dict(epi=api.Epilogue(0, bias=far(4).value)), dict(epi=api.Epilogue(0, mul=far(4).value)),   # (fp32 y over bf16 mul)
                 dict(epi=api.Epilogue(0, residual=far(4).value + 16))):
         assert forward(**bad) == api.EINVAL, bad
-    for bad in (dict(d_in=72), dict(d_out=36), dict(d_in=131088), dict(d_out=131080)):
+    for bad in (dict(d_in=72), dict(d_out=36), dict(d_in=131088), dict(d_out=131080), dict(T=2 ** 29 + 1)):
         assert forward(**bad) == api.EUNSUPPORTED, bad
     for name in ("x", "xs", "codes", "scale", "y", "ws"):
         assert forward(**{name: P(ODD)}) == api.EALIGN, name
@@ -87,7 +121,7 @@ def test_argument_errors_are_caught_before_launch():
     for bad in (dict(T=0), dict(dy=None), dict(codes=None), dict(scale=None), dict(dx=None), dict(dt=-1), dict(d_in=0), dict(dx=far(1)),
                 dict(dx=far(2)), dict(dx=far(3)), dict(r=P(far(4).value + 32))):
         assert backward(**bad) == api.EINVAL, bad
-    for bad in (dict(d_in=72), dict(d_out=36), dict(d_in=131088), dict(d_out=131080)):
+    for bad in (dict(d_in=72), dict(d_out=36), dict(d_in=131088), dict(d_out=131080), dict(T=2 ** 29 + 1)):
         assert backward(**bad) == api.EUNSUPPORTED, bad
     for name in ("dy", "codes", "scale", "r", "dx", "ws"):
         assert backward(**{name: P(ODD)}) == api.EALIGN, name
