@@ -159,7 +159,9 @@ _NATIVE_ENTRIES = (
     "qalora_shared_workspace_bytes", "qalora_forward_shared", "qalora_backward_shared", "qalora_swiglu_forward_wide",
     "qalora_swiglu_backward_wide", "qalora_forward_epilogue", "qalora_forward_deployed_epilogue",
     "qalora_epilogue_backward", "qalora_epilogue_backward_workspace_bytes", "qalora_muon_step",
-    "qalora_muon_workspace_bytes")
+    "qalora_muon_workspace_bytes", "qalora_quantize_tokens", "qalora_int8_workspace_bytes", "qalora_forward_int8",
+    "qalora_backward_int8", "qalora_kept8_bytes", "qalora_keep8", "qalora_swiglu_forward8", "qalora_swiglu_backward_kept8",
+    "qalora_epilogue_backward_kept8")
 
 
 def _bind_native():
@@ -1012,6 +1014,9 @@ def _given(t, name, dtype, shape, dev):
 def quantize_tokens(x, factor=None, q=None, s=None):
     """x bf16 [tokens, cols], each row in 8 bits with a scale of its own: (q int8 [tokens, cols], s fp32 [tokens]), what
     forward_int8 takes in place of x.  ``factor`` fp32 [cols] multiplies the columns first."""
+    out = _fast().quantize_tokens(x, factor, q, s)
+    if out is not None:
+        return out
     T, cols, dev = _matrix(x, "x", torch.bfloat16)
     _need(factor, "factor", torch.float32, (cols,), device=dev, optional=True)
     q, s = _given(q, "q", torch.int8, (T, cols), dev), _given(s, "s", torch.float32, (T,), dev)
@@ -1038,6 +1043,9 @@ def forward_int8(x, codes, scale, bias=None, act="none", mul=None, residual=None
     """y = act(s (q codes^T) scale + bias) * mul + residual in 8-bit integers (see qalora_forward_int8).  ``x`` is bf16
     [tokens, d_in], or what quantize_tokens or swiglu_forward_int8 made of one: (q, s).  The epilogue is forward_epilogue's.
     Returns y, or with ``keep_z`` (y, z)."""
+    out = _fast().forward_int8(x, codes, scale, bias, ACTIVATIONS.get(act), mul, residual, keep_z, out_dtype, ws, y, z)
+    if out is not None:
+        return out
     d_out, d_in, dev = _matrix(codes, "codes", torch.int8)
     _need(scale, "scale", torch.float32, (d_out,), device=dev)
     s = None
@@ -1070,6 +1078,9 @@ def forward_int8(x, codes, scale, bias=None, act="none", mul=None, residual=None
 def backward_int8(dy, codes, scale, residual=None, dx_dtype=torch.float32, ws=None, dx=None):
     """dx of forward_int8's product with the weight frozen (see qalora_backward_int8): dy bf16 [tokens, d_out] -> dx [tokens, d_in],
     plus ``residual`` (dx's type; it may be the ``dx`` that is passed: gradients of several linears then add up in place)."""
+    out = _fast().backward_int8(dy, codes, scale, residual, dx_dtype, ws, dx)
+    if out is not None:
+        return out
     d_out, d_in, dev = _matrix(codes, "codes", torch.int8)
     _need(scale, "scale", torch.float32, (d_out,), device=dev)
     _need(dy, "dy", torch.bfloat16, device=dev)
@@ -1102,6 +1113,9 @@ def _kept8(kept, name, tokens, cols, dev, new=False):
 
 def keep8(x, kept=None):
     """x bf16 [tokens, cols] kept in 8 bits for a backward (see qalora_keep8): an opaque uint8 tensor."""
+    out = _fast().keep8(x, kept)
+    if out is not None:
+        return out
     T, cols, dev = _matrix(x, "x", torch.bfloat16)
     kept = _kept8(kept, "kept", T, cols, dev, new=True)
     with _on(dev):
@@ -1129,6 +1143,9 @@ def _swiglu_input(gu, cols):
 
 def swiglu_forward_keep8(gu, cols, h=None, kept=None):
     """h = silu(gate) * up of gu = [gate | up] (bf16 [tokens, 2 cols]), and gate and up kept in 8 bits: (h, kept)."""
+    out = _fast().swiglu_forward_keep8(gu, cols, h, kept)
+    if out is not None:
+        return out
     T, dev = _swiglu_input(gu, cols)
     h = _given(h, "h", torch.bfloat16, (T, cols), dev)
     kept = _kept8(kept, "kept", 2 * T, cols, dev, new=True)
@@ -1141,6 +1158,9 @@ def swiglu_forward_keep8(gu, cols, h=None, kept=None):
 def swiglu_forward_int8(gu, cols, keep=False, q=None, s=None, kept=None, h=None):
     """silu(gate) * up of gu = [gate | up] as 8-bit tokens (q, s), what forward_int8 of the down projection takes; with
     ``keep`` ((q, s), kept), gate and up kept in 8 bits as by swiglu_forward_keep8.  A given ``h`` receives the hidden activations."""
+    out = _fast().swiglu_forward_int8(gu, cols, keep, q, s, kept, h)
+    if out is not None:
+        return out
     T, dev = _swiglu_input(gu, cols)
     q, s = _given(q, "q", torch.int8, (T, cols), dev), _given(s, "s", torch.float32, (T,), dev)
     _need(h, "h", torch.bfloat16, (T, cols), device=dev, optional=True)
@@ -1156,6 +1176,9 @@ def swiglu_forward_int8(gu, cols, keep=False, q=None, s=None, kept=None, h=None)
 
 def swiglu_backward_kept8(dh, kept, cols, dgu=None):
     """dgu = [dgate | dup] from dh (bf16 [tokens, cols]) and the gate and up that were kept in 8 bits."""
+    out = _fast().swiglu_backward_kept8(dh, kept, cols, dgu)
+    if out is not None:
+        return out
     T, width, dev = _matrix(dh, "dh", torch.bfloat16)
     if width != cols:
         raise ValueError(f"dh: shape {tuple(dh.shape)}, expected [tokens, {cols}]")
@@ -1170,6 +1193,9 @@ def swiglu_backward_kept8(dh, kept, cols, dgu=None):
 def epilogue_backward_kept8(dy, z8=None, act="none", mul8=None, want_dz=True, want_dbias=False, dz=None, dmul=None, dbias=None,
                             accumulate=False, ws=None):
     """epilogue_backward with z and mul as keep8 kept them: (dz, dmul, dbias), None in the place of what is not there."""
+    out = _fast().epilogue_backward_kept8(dy, z8, ACTIVATIONS.get(act), mul8, want_dz, want_dbias, dz, dmul, dbias, accumulate, ws)
+    if out is not None:
+        return out
     _need(dy, "dy")
     if dy.dim() != 2 or dy.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError(f"dy: {dy.dtype} {tuple(dy.shape)}, expected a float32 or bfloat16 matrix")

@@ -34,7 +34,9 @@ struct Library {
   X(qalora_forward_deployed) X(qalora_forward_factors16) X(qalora_adamw_step) X(qalora_shared_kept_bytes)             \
   X(qalora_shared_workspace_bytes) X(qalora_forward_shared) X(qalora_backward_shared) X(qalora_swiglu_forward_wide)   \
   X(qalora_swiglu_backward_wide) X(qalora_forward_epilogue) X(qalora_forward_deployed_epilogue)                        \
-  X(qalora_epilogue_backward) X(qalora_epilogue_backward_workspace_bytes) X(qalora_muon_step) X(qalora_muon_workspace_bytes)
+  X(qalora_epilogue_backward) X(qalora_epilogue_backward_workspace_bytes) X(qalora_muon_step) X(qalora_muon_workspace_bytes) \
+  X(qalora_quantize_tokens) X(qalora_int8_workspace_bytes) X(qalora_forward_int8) X(qalora_backward_int8) X(qalora_kept8_bytes) \
+  X(qalora_keep8) X(qalora_swiglu_forward8) X(qalora_swiglu_backward_kept8) X(qalora_epilogue_backward_kept8)
 #define QALORA_MEMBER(name) decltype(&::name) name = nullptr;
   QALORA_ENTRIES(QALORA_MEMBER)
 } lib;
@@ -147,6 +149,44 @@ struct Call {
       return at::empty({(int64_t)std::max<size_t>(size, 16)}, at::TensorOptions().dtype(at::kByte).device(dev));
     const at::Tensor* t = tensor(o);
     return t ? *t : at::Tensor();
+  }
+  // a bf16 matrix, from which the call takes its device
+  const at::Tensor* activations8(PyObject* o) {
+    const at::Tensor* t = tensor(o, true);
+    need(t && t->scalar_type() == at::kBFloat16 && t->dim() == 2 && t->size(0) > 0 && t->size(0) <= INT32_MAX && t->size(1) > 0 &&
+         t->size(1) <= INT32_MAX);
+    return ok ? t : nullptr;
+  }
+  void* vector(PyObject* o, int64_t n) {  // of fp32
+    const at::Tensor* t = tensor(o);
+    need(t && t->scalar_type() == at::kFloat && t->dim() == 1 && t->size(0) == n);
+    return ok ? t->data_ptr() : nullptr;
+  }
+  // the caller's, or new; one-dimensional where there is no second size
+  at::Tensor output(PyObject* o, at::ScalarType dtype, int64_t rows, int64_t cols = -1) {
+    if (!ok) return {};
+    if (o == Py_None) {
+      const auto opts = at::TensorOptions().dtype(dtype).device(dev);
+      return cols < 0 ? at::empty({rows}, opts) : at::empty({rows, cols}, opts);
+    }
+    const at::Tensor* t = tensor(o);
+    need(t && t->scalar_type() == dtype && t->dim() == (cols < 0 ? 1 : 2) && t->size(0) == rows && (cols < 0 || t->size(1) == cols));
+    return ok ? *t : at::Tensor();
+  }
+  // what was kept in 8 bits of [rows, cols]
+  void* kept8(PyObject* o, int64_t rows, int64_t cols) {
+    const at::Tensor* t = tensor(o);
+    need(t && t->scalar_type() == at::kByte && rows <= INT32_MAX);
+    const size_t size = ok ? lib.qalora_kept8_bytes((int)rows, (int)cols) : 0;
+    need(size > 0 && (size_t)t->nbytes() >= size);
+    return ok ? t->data_ptr() : nullptr;
+  }
+  at::Tensor kept8_output(PyObject* o, int64_t rows, int64_t cols) {
+    if (o != Py_None) return kept8(o, rows, cols) ? THPVariable_Unpack(o) : at::Tensor();
+    need(rows <= INT32_MAX);
+    const size_t size = ok ? lib.qalora_kept8_bytes((int)rows, (int)cols) : 0;
+    need(size > 0);
+    return ok ? at::empty({(int64_t)size}, at::TensorOptions().dtype(at::kByte).device(dev)) : at::Tensor();
   }
   // the call's device is the current one (elsewhere api.py makes it so first)
   void on_current_device() { need(ok && dev.index() == c10::hip::current_device()); }
@@ -610,17 +650,17 @@ FASTCALL(adamw_step, 9)
 FASTCALL_END
 
 // The epilogue of a forward whose output is `y`, [c.T, d_out] of type `code`.
-qalora_epilogue epilogue(Call& c, PyObject* bias, PyObject* act, PyObject* mul, PyObject* residual, int code) {
+qalora_epilogue epilogue(Call& c, int64_t d_out, PyObject* bias, PyObject* act, PyObject* mul, PyObject* residual, int code) {
   qalora_epilogue e{};
   e.act = c.integer(act);
   if (c.ok && bias != Py_None) {
     const at::Tensor* t = c.tensor(bias);
-    c.need(t && t->scalar_type() == at::kFloat && t->dim() == 1 && t->size(0) == c.desc.d_out);
+    c.need(t && t->scalar_type() == at::kFloat && t->dim() == 1 && t->size(0) == d_out);
     if (c.ok) e.bias = f32(t->data_ptr());
   }
-  if (c.ok && mul != Py_None) e.mul = c.matrix(mul, at::kBFloat16, c.T, c.desc.d_out);
+  if (c.ok && mul != Py_None) e.mul = c.matrix(mul, at::kBFloat16, c.T, d_out);
   if (c.ok && residual != Py_None)
-    e.residual = c.matrix(residual, code == QALORA_BF16 ? at::kBFloat16 : at::kFloat, c.T, c.desc.d_out);
+    e.residual = c.matrix(residual, code == QALORA_BF16 ? at::kBFloat16 : at::kFloat, c.T, d_out);
   return e;
 }
 
@@ -636,7 +676,7 @@ FASTCALL(forward_epilogue, 18)
   c.need((!keep || w.A) && (keep_z || a[16] == Py_None) && (keep || a[17] == Py_None));
   int code = 0;
   const at::Tensor y = c.out(a[15], a[13], c.T, c.desc.d_out, code);
-  qalora_epilogue e = epilogue(c, a[7], a[8], a[9], a[10], code);
+  qalora_epilogue e = epilogue(c, c.desc.d_out, a[7], a[8], a[9], a[10], code);
   PLAIN(c);
   at::Tensor z, kept;
   if (keep_z) {
@@ -677,7 +717,7 @@ FASTCALL(forward_deployed_epilogue, 11)
     packed = c.bytes(a[3], c.T > QALORA_DEPLOYED_STREAM_TOKENS ? lib.qalora_packed_bytes(&c.desc) : 0);
   int code = 0;
   const at::Tensor y = c.out(a[10], a[8], c.T, c.desc.d_out, code);
-  const qalora_epilogue e = epilogue(c, a[4], a[5], a[6], a[7], code);
+  const qalora_epilogue e = epilogue(c, c.desc.d_out, a[4], a[5], a[6], a[7], code);
   PLAIN(c);
   const at::Tensor ws = c.scratch(a[9], a[9] == Py_None ? lib.qalora_workspace_bytes(&c.desc, (int)c.T, QALORA_OP_FORWARD) : 0);
   PLAIN(c);
@@ -688,8 +728,8 @@ FASTCALL(forward_deployed_epilogue, 11)
   return given_or(a[10], y);
 FASTCALL_END
 
-// dy, z, act, mul, want_dz, want_dbias, dz, dmul, dbias, accumulate, ws
-FASTCALL(epilogue_backward, 11)
+// dy, z, act, mul, want_dz, want_dbias, dz, dmul, dbias, accumulate, ws; kept8: z and mul are what keep8 made of them
+PyObject* epilogue_backward_of(PyObject* const* a, bool kept8) {
   Call c;
   const at::Tensor* dy = c.tensor(a[0], true);
   c.need(dy && dy->dim() == 2 && dy->size(0) > 0 && dy->size(0) <= INT32_MAX && dy->size(1) > 0 && dy->size(1) <= INT32_MAX);
@@ -697,9 +737,10 @@ FASTCALL(epilogue_backward, 11)
   PLAIN(c);
   const int dtype = c.dtype_of(dy->scalar_type());
   const int64_t T = dy->size(0), cols = dy->size(1);
-  void* z = a[1] != Py_None ? c.matrix(a[1], at::kBFloat16, T, cols) : nullptr;
+  auto operand = [&](PyObject* o) { return kept8 ? c.kept8(o, T, cols) : c.matrix(o, at::kBFloat16, T, cols); };
+  void* z = a[1] != Py_None ? operand(a[1]) : nullptr;
   const int act = c.integer(a[2]);
-  void* mul = a[3] != Py_None ? c.matrix(a[3], at::kBFloat16, T, cols) : nullptr;
+  void* mul = a[3] != Py_None ? operand(a[3]) : nullptr;
   const bool want_dz = c.truth(a[4]), want_dbias = c.truth(a[5]), acc = c.truth(a[9]);
   c.need(a[7] == Py_None || mul);
   if (a[6] != Py_None) c.matrix(a[6], at::kBFloat16, T, cols);
@@ -729,11 +770,195 @@ FASTCALL(epilogue_backward, 11)
   void *p_dy = dy->data_ptr(), *p_dz = data(dz), *p_dmul = data(dmul), *p_ws = data(ws);
   float* p_dbias = f32(data(dbias));
   void* st = stream();
-  if (!run("qalora_epilogue_backward", lib.qalora_epilogue_backward, act, (int)T, (int)cols, p_dy, dtype, z, mul, p_dz, p_dmul,
+  if (!run(kept8 ? "qalora_epilogue_backward_kept8" : "qalora_epilogue_backward",
+           kept8 ? lib.qalora_epilogue_backward_kept8 : lib.qalora_epilogue_backward, act, (int)T, (int)cols, p_dy, dtype, z, mul, p_dz, p_dmul,
            p_dbias, acc ? 1 : 0, p_ws, ws.defined() ? ws.nbytes() : 0, st))
     return nullptr;
   auto back = [](PyObject* o, const at::Tensor& t) { return t.defined() ? given_or(o, t) : Py_NewRef(Py_None); };
   return tuple({back(a[6], dz), back(a[7], dmul), back(a[8], dbias)});
+}
+FASTCALL(epilogue_backward, 11)
+  return epilogue_backward_of(a, false);
+FASTCALL_END
+FASTCALL(epilogue_backward_kept8, 11)
+  return epilogue_backward_of(a, true);
+FASTCALL_END
+
+// x, factor, q, s
+FASTCALL(quantize_tokens, 4)
+  Call c;
+  const at::Tensor* x = c.activations8(a[0]);
+  c.on_current_device();
+  PLAIN(c);
+  const int64_t T = x->size(0), cols = x->size(1);
+  float* factor = a[1] != Py_None ? f32(c.vector(a[1], cols)) : nullptr;
+  const at::Tensor q = c.output(a[2], at::kChar, T, cols), s = c.output(a[3], at::kFloat, T);
+  PLAIN(c);
+  void* st = stream();
+  if (!run("qalora_quantize_tokens", lib.qalora_quantize_tokens, (int)T, (int)cols, x->data_ptr(), factor,
+           static_cast<int8_t*>(q.data_ptr()), f32(s.data_ptr()), st))
+    return nullptr;
+  return tuple({given_or(a[2], q), given_or(a[3], s)});
+FASTCALL_END
+
+// The weight's codes [d_out, d_in] and scales, from which the call takes its device.
+struct Weight8 {
+  int8_t* codes = nullptr;
+  float* scale = nullptr;
+  int64_t d_out = 0, d_in = 0;
+};
+Weight8 weight8(Call& c, PyObject* codes, PyObject* scale) {
+  Weight8 w;
+  const at::Tensor* t = c.tensor(codes, true);
+  c.need(t && t->scalar_type() == at::kChar && t->dim() == 2 && t->size(0) > 0 && t->size(0) <= INT32_MAX && t->size(1) > 0 &&
+         t->size(1) <= INT32_MAX);
+  if (!c.ok) return w;
+  w.d_out = t->size(0);
+  w.d_in = t->size(1);
+  w.codes = static_cast<int8_t*>(t->data_ptr());
+  w.scale = f32(c.vector(scale, w.d_out));
+  return w;
+}
+
+// x or (q, s), codes, scale, bias, act, mul, residual, keep_z, out_dtype, ws, y, z
+FASTCALL(forward_int8, 12)
+  Call c;
+  const Weight8 w = weight8(c, a[1], a[2]);
+  c.on_current_device();
+  PLAIN(c);
+  PyObject *px = a[0], *ps = nullptr;
+  if (PyTuple_CheckExact(px)) {
+    if (PyTuple_GET_SIZE(px) != 2) Py_RETURN_NONE;
+    ps = PyTuple_GET_ITEM(px, 1);
+    px = PyTuple_GET_ITEM(px, 0);
+  }
+  const at::Tensor* x = c.tensor(px);
+  c.need(x && x->scalar_type() == (ps ? at::kChar : at::kBFloat16) && x->dim() == 2 && x->size(0) > 0 && x->size(0) <= INT32_MAX &&
+         x->size(1) == w.d_in);
+  PLAIN(c);
+  c.T = x->size(0);
+  float* s = ps ? f32(c.vector(ps, c.T)) : nullptr;
+  const bool keep_z = c.truth(a[7]);
+  c.need(keep_z || a[11] == Py_None);
+  int code = 0;
+  const at::Tensor y = c.out(a[10], a[8], c.T, w.d_out, code);
+  qalora_epilogue e = epilogue(c, w.d_out, a[3], a[4], a[5], a[6], code);
+  PLAIN(c);
+  at::Tensor z;
+  if (keep_z) {
+    z = c.output(a[11], at::kBFloat16, c.T, w.d_out);
+    PLAIN(c);
+    e.z = z.data_ptr();
+  }
+  const at::Tensor ws = c.scratch(a[9], a[9] == Py_None ? lib.qalora_int8_workspace_bytes((int)c.T, (int)w.d_in, (int)w.d_out, QALORA_OP_FORWARD) : 0);
+  PLAIN(c);
+  void* st = stream();
+  if (!run("qalora_forward_int8", lib.qalora_forward_int8, (int)c.T, (int)w.d_in, (int)w.d_out, x->data_ptr(), s, w.codes, w.scale,
+           &e, y.data_ptr(), code, ws.data_ptr(), ws.nbytes(), st))
+    return nullptr;
+  if (!keep_z) return given_or(a[10], y);
+  return tuple({given_or(a[10], y), given_or(a[11], z)});
+FASTCALL_END
+
+// dy, codes, scale, residual, dx_dtype, ws, dx
+FASTCALL(backward_int8, 7)
+  Call c;
+  const Weight8 w = weight8(c, a[1], a[2]);
+  c.on_current_device();
+  const at::Tensor* dy = c.tensor(a[0]);
+  c.need(dy && dy->scalar_type() == at::kBFloat16 && dy->dim() == 2 && dy->size(0) > 0 && dy->size(0) <= INT32_MAX && dy->size(1) == w.d_out);
+  PLAIN(c);
+  c.T = dy->size(0);
+  int code = 0;
+  const at::Tensor dx = c.out(a[6], a[4], c.T, w.d_in, code);
+  void* residual = a[3] != Py_None ? c.matrix(a[3], code == QALORA_BF16 ? at::kBFloat16 : at::kFloat, c.T, w.d_in) : nullptr;
+  PLAIN(c);
+  const at::Tensor ws = c.scratch(a[5], a[5] == Py_None ? lib.qalora_int8_workspace_bytes((int)c.T, (int)w.d_in, (int)w.d_out, QALORA_OP_BACKWARD) : 0);
+  PLAIN(c);
+  void* st = stream();
+  if (!run("qalora_backward_int8", lib.qalora_backward_int8, (int)c.T, (int)w.d_in, (int)w.d_out, dy->data_ptr(), w.codes, w.scale,
+           residual, dx.data_ptr(), code, ws.data_ptr(), ws.nbytes(), st))
+    return nullptr;
+  return given_or(a[6], dx);
+FASTCALL_END
+
+// x, kept
+FASTCALL(keep8, 2)
+  Call c;
+  const at::Tensor* x = c.activations8(a[0]);
+  c.on_current_device();
+  PLAIN(c);
+  const int64_t T = x->size(0), cols = x->size(1);
+  const at::Tensor kept = c.kept8_output(a[1], T, cols);
+  PLAIN(c);
+  void* st = stream();
+  if (!run("qalora_keep8", lib.qalora_keep8, (int)T, (int)cols, x->data_ptr(), kept.data_ptr(), st)) return nullptr;
+  return given_or(a[1], kept);
+FASTCALL_END
+
+// gu [T, 2 cols] of a SwiGLU, and cols
+const at::Tensor* swiglu_input(Call& c, PyObject* gu, PyObject* pcols, int64_t& cols) {
+  const at::Tensor* t = c.activations8(gu);
+  cols = c.integer(pcols);
+  c.on_current_device();
+  c.need(c.ok && cols > 0 && t->size(1) == 2 * cols && t->size(0) < (1 << 30));
+  return c.ok ? t : nullptr;
+}
+
+// gu, cols, h, kept
+FASTCALL(swiglu_forward_keep8, 4)
+  Call c;
+  int64_t cols = 0;
+  const at::Tensor* gu = swiglu_input(c, a[0], a[1], cols);
+  PLAIN(c);
+  const int64_t T = gu->size(0);
+  const at::Tensor h = c.output(a[2], at::kBFloat16, T, cols), kept = c.kept8_output(a[3], 2 * T, cols);
+  PLAIN(c);
+  void* st = stream();
+  if (!run("qalora_swiglu_forward8", lib.qalora_swiglu_forward8, (int)T, (int)cols, gu->data_ptr(), h.data_ptr(), nullptr, nullptr,
+           kept.data_ptr(), st))
+    return nullptr;
+  return tuple({given_or(a[2], h), given_or(a[3], kept)});
+FASTCALL_END
+
+// gu, cols, keep, q, s, kept, h
+FASTCALL(swiglu_forward_int8, 7)
+  Call c;
+  int64_t cols = 0;
+  const at::Tensor* gu = swiglu_input(c, a[0], a[1], cols);
+  const bool keep = c.truth(a[2]);
+  c.need(keep || a[5] == Py_None);
+  PLAIN(c);
+  const int64_t T = gu->size(0);
+  const at::Tensor q = c.output(a[3], at::kChar, T, cols), s = c.output(a[4], at::kFloat, T);
+  at::Tensor kept;
+  if (keep) kept = c.kept8_output(a[5], 2 * T, cols);
+  void* h = a[6] != Py_None ? c.matrix(a[6], at::kBFloat16, T, cols) : nullptr;
+  PLAIN(c);
+  void* st = stream();
+  if (!run("qalora_swiglu_forward8", lib.qalora_swiglu_forward8, (int)T, (int)cols, gu->data_ptr(), h, static_cast<int8_t*>(q.data_ptr()),
+           f32(s.data_ptr()), keep ? kept.data_ptr() : nullptr, st))
+    return nullptr;
+  PyObject* tokens = tuple({given_or(a[3], q), given_or(a[4], s)});
+  return keep ? tuple({tokens, given_or(a[5], kept)}) : tokens;
+FASTCALL_END
+
+// dh, kept, cols, dgu
+FASTCALL(swiglu_backward_kept8, 4)
+  Call c;
+  const at::Tensor* dh = c.activations8(a[0]);
+  const int64_t cols = c.integer(a[2]);
+  c.on_current_device();
+  c.need(c.ok && dh->size(1) == cols && dh->size(0) < (1 << 30));
+  PLAIN(c);
+  const int64_t T = dh->size(0);
+  void* kept = c.kept8(a[1], 2 * T, cols);
+  const at::Tensor dgu = c.output(a[3], at::kBFloat16, T, 2 * cols);
+  PLAIN(c);
+  void* st = stream();
+  if (!run("qalora_swiglu_backward_kept8", lib.qalora_swiglu_backward_kept8, (int)T, (int)cols, dh->data_ptr(), kept, dgu.data_ptr(), st))
+    return nullptr;
+  return given_or(a[3], dgu);
 FASTCALL_END
 
 // hp, params, grads, momentum, zero_grads, ws -> True
@@ -805,7 +1030,9 @@ PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr}, METHOD(quantize)
                          METHOD(backward), METHOD(backward_kept), METHOD(forward_deployed), METHOD(forward_factors16),
                          METHOD(forward_shared), METHOD(backward_shared), METHOD(swiglu_forward_wide),
                          METHOD(swiglu_backward_wide), METHOD(adamw_step), METHOD(forward_epilogue), METHOD(forward_deployed_epilogue),
-                         METHOD(epilogue_backward), METHOD(muon_step), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(epilogue_backward), METHOD(muon_step), METHOD(epilogue_backward_kept8), METHOD(quantize_tokens),
+                         METHOD(forward_int8), METHOD(backward_int8), METHOD(keep8), METHOD(swiglu_forward_keep8),
+                         METHOD(swiglu_forward_int8), METHOD(swiglu_backward_kept8), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Native form of the binding's calls (see api.py).", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

@@ -27,7 +27,7 @@ struct RowScale {
   float s;    // as stored: NaN for a row with an infinity or a NaN, then all codes are 0
   float up;   // v and s times this power of two are ordinary numbers whatever the row's magnitude
   float by;   // s * up
-  float inv;  // 1 / by, 0 for a row of zeros
+  float inv;  // 1 / by, 0 for a row without a scale
 };
 // `top`: the bits of the row's largest magnitude (as integers those of finite values, infinities and NaNs come in that order)
 __device__ __forceinline__ RowScale row_scale_of(uint32_t top) {
@@ -40,25 +40,36 @@ __device__ __forceinline__ RowScale row_scale_of(uint32_t top) {
   r.inv = r.by > 0.0f ? 1.0f / r.by : 0.0f;
   return r;
 }
-// The code of v, as the float whose low byte it is.  v inv is off by at most 127 2^-23 = 1.6e-5 from the quotient, so rounding it can go
-// wrong only that close to the middle between two codes; there the remainder v - code s, which fp32 holds exactly (it is a multiple
-// of the smaller of the last places of v and s, and at most about s / 2), says which side v is on.
-__device__ __forceinline__ float row_code(float v, const RowScale& r) {
-  v *= r.up;
-  const float t = v * r.inv;
+// The codes of eight v.  v inv is off by at most 127 2^-23 = 1.6e-5 from the quotient, so rounding it can go wrong only that close to the
+// middle between two codes; there the remainder v - code s, which fp32 holds exactly (it is a multiple of the smaller of the last
+// places of v and s, and at most about s / 2), says which side v is on.  (A quotient is past 127 only where s is subnormal.)
+__device__ __forceinline__ float exact_code(float v, float t, const RowScale& r) {
   float q = __builtin_rintf(t);
-  if (__builtin_fabsf(t - q) > 0.49995f) {
-    const float left = __builtin_fmaf(-q, r.by, v), twice = __builtin_fabsf(left) + __builtin_fabsf(left);
-    const bool odd = ((int)q & 1) != 0;
-    if (twice > r.by || (twice == r.by && odd)) q += left > 0.0f ? 1.0f : -1.0f;
-  }
-  return __builtin_amdgcn_fmed3f(q, -127.0f, 127.0f) + kWhole;  // (past 127 only where s is subnormal)
+  const float left = __builtin_fmaf(-q, r.by, v), twice = __builtin_fabsf(left) + __builtin_fabsf(left);
+  const bool odd = ((int)q & 1) != 0;
+  if (twice > r.by || (twice == r.by && odd)) q += left > 0.0f ? 1.0f : -1.0f;
+  return __builtin_amdgcn_fmed3f(q, -127.0f, 127.0f) + kWhole;
 }
 __device__ __forceinline__ u8x8 row_codes(const float (&v)[8], const RowScale& r) {
+  float t[8], f[8], worst = 0.0f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    t[k] = v[k] * r.inv;
+    f[k] = t[k] + kWhole;  // the code in its low byte
+    worst = fmaxf(worst, __builtin_fabsf(t[k] - (f[k] - kWhole)));
+  }
+  if (worst > 0.49995f || r.up != 1.0f) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float w = v[k] * r.up;
+      f[k] = exact_code(w, w * r.inv, r);
+    }
+  }
   uint32_t c[8];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) c[k] = r.inv > 0.0f ? __float_as_uint(row_code(v[k], r)) : 0u;
-  return u8x8{low_bytes(c[0], c[1], c[2], c[3]), low_bytes(c[4], c[5], c[6], c[7])};
+  for (int k = 0; k < 8; ++k) c[k] = __float_as_uint(f[k]);
+  const uint32_t mask = r.inv > 0.0f ? 0xffffffffu : 0u;  // (no scale: codes 0)
+  return u8x8{low_bytes(c[0], c[1], c[2], c[3]) & mask, low_bytes(c[4], c[5], c[6], c[7]) & mask};
 }
 
 // ---- 32 neighbouring columns share an exponent ---------------------------------------------------------------------------

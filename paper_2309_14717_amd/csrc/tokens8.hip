@@ -96,7 +96,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void tokens8_kernel(cons
 }
 
 hipError_t launch_tokens8(const Tokens8Args& args, hipStream_t st) {
-  const Tokens8Plan plan = tokens8_plan(args.ld);
+  const Tokens8Plan plan = tokens8_plan(args.rows, args.ld);
   Tokens8Args a = args;
   auto go = [&](auto from_c) {
     constexpr int FROM = decltype(from_c)::value;
@@ -106,7 +106,12 @@ hipError_t launch_tokens8(const Tokens8Args& args, hipStream_t st) {
       case 6402: tokens8_kernel<64, 2, FROM><<<blocks, 256, 0, st>>>(a); break;
       case 25601: tokens8_kernel<256, 1, FROM><<<blocks, 256, 0, st>>>(a); break;
       case 25602: tokens8_kernel<256, 2, FROM><<<blocks, 256, 0, st>>>(a); break;
+      case 25603: tokens8_kernel<256, 3, FROM><<<blocks, 256, 0, st>>>(a); break;
       case 25604: tokens8_kernel<256, 4, FROM><<<blocks, 256, 0, st>>>(a); break;
+      case 25606: tokens8_kernel<256, 6, FROM><<<blocks, 256, 0, st>>>(a); break;
+      case 25608: tokens8_kernel<256, 8, FROM><<<blocks, 256, 0, st>>>(a); break;
+      case 25612: tokens8_kernel<256, 12, FROM><<<blocks, 256, 0, st>>>(a); break;
+      case 102401: tokens8_kernel<1024, 1, FROM><<<blocks, 1024, 0, st>>>(a); break;
       case 102402: tokens8_kernel<1024, 2, FROM><<<blocks, 1024, 0, st>>>(a); break;
       case 102404: tokens8_kernel<1024, 4, FROM><<<blocks, 1024, 0, st>>>(a); break;
       case 102408: tokens8_kernel<1024, 8, FROM><<<blocks, 1024, 0, st>>>(a); break;
@@ -171,8 +176,10 @@ __global__ __launch_bounds__(256) void weight8_codes_kernel(const Weight8Args p)
   const int c = threadIdx.x % 64, j = blockIdx.x * 64 + c, i0 = blockIdx.y * 64;
   if (j < p.d_out) {
     const RowScale r = row_scale_of(reinterpret_cast<const uint32_t*>(p.scale)[j]);
-    for (int k = threadIdx.x / 64; k < 64 && i0 + k < p.d_in; k += 4)
-      tile[c][k] = r.inv > 0.0f ? (uint8_t)__float_as_uint(row_code(weight_at<NBITS>(p, i0 + k, j), r)) : (uint8_t)0;
+    for (int k = threadIdx.x / 64; k < 64 && i0 + k < p.d_in; k += 4) {
+      const float w = weight_at<NBITS>(p, i0 + k, j) * r.up;
+      tile[c][k] = r.inv > 0.0f ? (uint8_t)__float_as_uint(exact_code(w, w * r.inv, r)) : (uint8_t)0;
+    }
   }
   __syncthreads();
   const int t = threadIdx.x / 16, q = threadIdx.x % 16;  // sixteen lanes a channel, four rows each

@@ -11,8 +11,11 @@ pytestmark = pytest.mark.gpu
 
 @pytest.mark.parametrize("cols", [8, 24, 264, 1000, 1024, 1032, 2048, 4096, 5000, 8192, 8200, 11008, 22016, 32768, 40000, 65536, 131072])
 @pytest.mark.parametrize("scaled", [False, True])
-def test_tokens(gpu_api, cols, scaled):
+@pytest.mark.parametrize("many", [False, True])  # the launch has another shape for more than 512 rows
+def test_tokens(gpu_api, cols, scaled, many):
     T = 7 if cols < 30000 else 3
+    if many:
+        T = 515 if cols < 30000 else 513
     x = ic.drawn_tokens(cols, T, cols)
     x[1] = 0
     x[2, :] = 0

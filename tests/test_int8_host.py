@@ -14,8 +14,8 @@ SOURCE = r"""
 #include "int8.hpp"
 #include "tokens8_plan.hpp"
 using namespace qalora;
-extern "C" void tokens(int cols, int* o) {
-  const Tokens8Plan p = tokens8_plan(cols);
+extern "C" void tokens(int rows, int cols, int* o) {
+  const Tokens8Plan p = tokens8_plan(rows, cols);
   o[0] = p.lanes; o[1] = p.pieces; o[2] = p.rows;
 }
 extern "C" void product(int M, int N, int K, int back, int* o) {
@@ -41,11 +41,12 @@ def host(tmp_path_factory):
 def test_rows_are_covered(host):
     o = (ctypes.c_int * 3)()
     for cols in list(range(8, 20000, 8)) + list(range(20000, 131073, 24)) + [131072]:
-        host.tokens(cols, o)
-        lanes, pieces, rows = o
-        assert lanes * pieces * 8 >= cols and (lanes, pieces) in {(64, 1), (64, 2), (256, 1), (256, 2), (256, 4), (1024, 2), (1024, 4),
-                                                                  (1024, 8), (1024, 16)}
-        assert rows == (4 if lanes == 64 else 1)
+        for rows_in in (1, 512, 513, 100000):
+            host.tokens(rows_in, cols, o)
+            lanes, pieces, rows = o
+            assert lanes * pieces * 8 >= cols and (lanes, pieces) in {(64, 1), (64, 2), (256, 1), (256, 2), (256, 3), (256, 4), (256, 6), (256, 8),
+                                                                      (256, 12), (1024, 1), (1024, 2), (1024, 4), (1024, 8), (1024, 16)}
+            assert rows == (4 if lanes == 64 else 1)
 
 
 def test_product_plans(host):
