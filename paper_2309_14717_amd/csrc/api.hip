@@ -1023,7 +1023,7 @@ int qalora_swiglu_forward8(int tokens, int cols, const void* gu, void* h, int8_t
     a.cols = a.ld = cols;
     a.from = TOKENS8_SWIGLU;
     e = launch_tokens8(a, as_stream(stream));
-  } else if (kept) {
+  } else {
     Swiglu8Args a{};
     a.gu = static_cast<uint16_t*>(const_cast<void*>(gu));
     a.h = static_cast<uint16_t*>(h);
@@ -1031,8 +1031,6 @@ int qalora_swiglu_forward8(int tokens, int cols, const void* gu, void* h, int8_t
     a.rows = tokens;
     a.cols = cols;
     e = launch_swiglu_keep8(a, as_stream(stream));
-  } else {
-    e = launch_swiglu_forward_wide(gu, h, tokens, cols, as_stream(stream));
   }
   return e == hipSuccess ? QALORA_OK : QALORA_EHIP;
 }

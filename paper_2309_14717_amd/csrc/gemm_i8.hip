@@ -303,6 +303,16 @@ __global__ __launch_bounds__(WM* WN * 64) void gemm_i8_kernel(const Int8GemmArgs
     bias[0] = reinterpret_cast<const f32x4*>(p.epi.bias + col)[0];
     bias[1] = reinterpret_cast<const f32x4*>(p.epi.bias + col)[1];
   }
+  // The other operands of a thread's next rows are asked for while the rows before are finished.
+  constexpr int ROWS = ceil_div(PB * 16, ROWS_AT_ONCE), BATCH = ROWS % 4 == 0 ? 4 : ROWS % 3 == 0 ? 3 : ROWS % 2 == 0 ? 2 : 1;
+  // (a thread's rows of a pass; how many are on their way)
+  EpilogueOperands coming[BATCH];
+  auto ask = [&](int pass, int row, EpilogueOperands& o) {
+    const int rl = row_in + row * ROWS_AT_ONCE, m = m0 + (wm * TM + pass * PB) * 16 + rl;
+    if (col_ok && rl < PB * 16 && m < p.M) request_operands(p.epi, (size_t)m * p.N + col, p.out_bf16, o);
+  };
+#pragma unroll
+  for (int k = 0; k < BATCH; ++k) ask(0, k, coming[k]);
 #pragma unroll
   for (int pass = 0; pass < TM / PB; ++pass) {
 #pragma unroll
@@ -317,30 +327,31 @@ __global__ __launch_bounds__(WM* WN * 64) void gemm_i8_kernel(const Int8GemmArgs
       }
     }
     const int base = m0 + (wm * TM + pass * PB) * 16;
-    EpilogueOperands coming{};
-    auto ask = [&](int rl) {
-      if (col_ok && rl < PB * 16 && base + rl < p.M) request_operands(p.epi, (size_t)(base + rl) * p.N + col, p.out_bf16, coming);
-    };
-    ask(row_in);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma nounroll
-    for (int rl = row_in; rl < PB * 16; rl += ROWS_AT_ONCE) {
-      const EpilogueOperands now = coming;
-      ask(rl + ROWS_AT_ONCE);
-      const char* src = stage_lds + rl * CW * 4;
-      const f32x4 s0 = *reinterpret_cast<const f32x4*>(src + (((2 * ch) ^ (rl & MASK)) << 4)) + bias[0];
-      const f32x4 s1 = *reinterpret_cast<const f32x4*>(src + (((2 * ch + 1) ^ (rl & MASK)) << 4)) + bias[1];
-      if (!col_ok || base + rl >= p.M) continue;
-      const size_t at = (size_t)(base + rl) * p.N + col;
-      float v[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
-      apply_epilogue8(p.epi, now, v, at, p.out_bf16);
-      if (p.out_bf16) {
-        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + at) =
-            uint4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
-      } else {
-        f32x4* o = reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at);
-        o[0] = f32x4{v[0], v[1], v[2], v[3]};
-        o[1] = f32x4{v[4], v[5], v[6], v[7]};
+    for (int first = 0; first < ROWS; first += BATCH) {
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        const EpilogueOperands now = coming[k];
+        const int next = first + k + BATCH;
+        if (next < ROWS) ask(pass, next, coming[k]);
+        else if (pass + 1 < TM / PB) ask(pass + 1, next - ROWS, coming[k]);
+        const int rl = row_in + (first + k) * ROWS_AT_ONCE;
+        if (!col_ok || rl >= PB * 16 || base + rl >= p.M) continue;
+        const char* src = stage_lds + rl * CW * 4;
+        const f32x4 s0 = *reinterpret_cast<const f32x4*>(src + (((2 * ch) ^ (rl & MASK)) << 4)) + bias[0];
+        const f32x4 s1 = *reinterpret_cast<const f32x4*>(src + (((2 * ch + 1) ^ (rl & MASK)) << 4)) + bias[1];
+        const size_t at = (size_t)(base + rl) * p.N + col;
+        float v[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
+        apply_epilogue8(p.epi, now, v, at, p.out_bf16);
+        if (p.out_bf16) {
+          *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + at) =
+              uint4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+        } else {
+          f32x4* o = reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at);
+          o[0] = f32x4{v[0], v[1], v[2], v[3]};
+          o[1] = f32x4{v[4], v[5], v[6], v[7]};
+        }
       }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the pass has been read out

@@ -2,6 +2,7 @@
 // that share an exponent (kept activations).
 #pragma once
 #include "common.hpp"
+#include "epilogue.hpp"
 
 namespace qalora {
 
@@ -19,6 +20,18 @@ __device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c
 __device__ __forceinline__ float code_value(uint32_t word, int byte) { return (float)(int8_t)(word >> (8 * byte)); }
 __device__ __forceinline__ float bf16_of(const u16x8& w, int k) {
   return __uint_as_float((k & 1) ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16);
+}
+
+// silu(gate) * up of eight columns.  (The hardware's reciprocal: with a division rows of hidden activations to 8 bits are bound by their
+// arithmetic.)
+__device__ __forceinline__ u16x8 swiglu8(const u16x8& g, const u16x8& u) {
+  u16x8 h;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float g0 = bf16_of(g, 2 * k), g1 = bf16_of(g, 2 * k + 1);
+    h[k] = pack_bf16x2(g0 * logistic(g0) * bf16_of(u, 2 * k), g1 * logistic(g1) * bf16_of(u, 2 * k + 1));
+  }
+  return h;
 }
 
 // ---- one scale a row: s = fl32(top / 127), code = rne(v / s) of the exact quotient -----------------------------------

@@ -60,7 +60,7 @@ __global__ __launch_bounds__(256) void restore8_kernel(const Keep8Args p) {
   }
 }
 
-// gu = [gate | up] is [2 rows, cols] to what keeps it: a token's gate is row 2t, its up row 2t + 1.
+// (h or what is kept may be left out.)  gu = [gate | up] is [2 rows, cols] to what keeps it: a token's gate is row 2t, its up row 2t + 1.
 __global__ __launch_bounds__(256) void swiglu_keep8_kernel(const Swiglu8Args p) {
   const int eights = p.cols / 8, per_row = round_up(eights, 4);
   const size_t groups = keep8_groups(p.cols);
@@ -74,11 +74,8 @@ __global__ __launch_bounds__(256) void swiglu_keep8_kernel(const Swiglu8Args p) 
     }
     const uint32_t eg = group_exponent(g), eu = group_exponent(u);
     if (i.at >= eights) continue;
-    u16x8 h;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      h[k] = pack_bf16x2(swiglu_value(bf16_of(g, 2 * k), bf16_of(u, 2 * k)), swiglu_value(bf16_of(g, 2 * k + 1), bf16_of(u, 2 * k + 1)));
-    reinterpret_cast<u16x8*>(p.h)[i.row * eights + i.at] = h;
+    if (p.h) reinterpret_cast<u16x8*>(p.h)[i.row * eights + i.at] = swiglu8(g, u);
+    if (!p.kept) continue;
     reinterpret_cast<u8x8*>(p.kept)[at] = group_codes(g, eg);
     reinterpret_cast<u8x8*>(p.kept)[at + eights] = group_codes(u, eu);
     if (i.at % 4 == 0) {

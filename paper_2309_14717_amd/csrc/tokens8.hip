@@ -5,7 +5,6 @@
 // largest magnitude is known.  Bound by its bytes, 3 a column (SwiGLU: 5, and 2 more with the kept halves).
 #include "int8.hpp"
 #include "kernels.hpp"
-#include "swiglu.hpp"
 #include "tokens8_plan.hpp"
 
 namespace qalora {
@@ -17,80 +16,131 @@ __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(
 template <int LANES, int PIECES, int FROM>
 __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void tokens8_kernel(const Tokens8Args p) {
   constexpr int WAVES = LANES / 64;
-  const int lane = threadIdx.x % LANES;
-  const size_t row = (size_t)p.row_begin + (LANES == 64 ? blockIdx.x * 4 + threadIdx.x / 64 : blockIdx.x);
-  if (LANES == 64 && row >= (size_t)p.row_end) return;
-  const int eights = p.cols / 8;
-  auto values = [&](const u16x8& w, int at, float (&v)[8]) {
+  constexpr bool HOLD = LANES < 1024 || PIECES <= (FROM == TOKENS8_SWIGLU ? 4 : 8);  // (else a row is read twice)
+  const int lane = threadIdx.x % LANES, eights = p.cols / 8;
+  // The factors of a thread's columns, for all rows it comes to: read for each row they would be more bytes than the row.
+  // (Where they are too many for the registers, of rows beyond 16384 columns, they are.)
+  constexpr bool KEEP = FROM == TOKENS8_SCALED && PIECES * 8 <= 64 && LANES < 1024;
+  f32x4 factor[KEEP ? PIECES : 1][2];
+  if constexpr (KEEP)
+#pragma unroll
+    for (int q = 0; q < PIECES; ++q) {
+      const int at = lane + q * LANES;
+      factor[q][0] = factor[q][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      if (at < eights) {
+        factor[q][0] = reinterpret_cast<const f32x4*>(p.factor)[2 * at];
+        factor[q][1] = reinterpret_cast<const f32x4*>(p.factor)[2 * at + 1];
+      }
+    }
+  auto values = [&](const u16x8& w, int q, float (&v)[8]) {
     f32x4 f[2];
-    if (FROM == TOKENS8_SCALED) {
-      f[0] = reinterpret_cast<const f32x4*>(p.factor)[2 * at];
-      f[1] = reinterpret_cast<const f32x4*>(p.factor)[2 * at + 1];
+    if constexpr (KEEP && HOLD) {
+      f[0] = factor[q][0];
+      f[1] = factor[q][1];
+    } else if (FROM == TOKENS8_SCALED && lane + q * LANES < eights) {
+      f[0] = reinterpret_cast<const f32x4*>(p.factor)[2 * (lane + q * LANES)];
+      f[1] = reinterpret_cast<const f32x4*>(p.factor)[2 * (lane + q * LANES) + 1];
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = FROM == TOKENS8_SCALED ? bf16_of(w, k) * f[k >> 2][k & 3] : bf16_of(w, k);
   };
 
-  u16x8 held[PIECES];
-  uint32_t top = 0;
-#pragma unroll
-  for (int q = 0; q < PIECES; ++q) {
+  struct Columns {  // eight of a row: as they are, or gate and up
+    u16x8 x, up;
+  };
+  auto load = [&](size_t row, int q) {
     const int at = lane + q * LANES;
-    held[q] = u16x8{0, 0, 0, 0};
-    if (FROM == TOKENS8_SWIGLU) {
-      u16x8 g{0, 0, 0, 0}, u{0, 0, 0, 0};
+    Columns c{u16x8{0, 0, 0, 0}, u16x8{0, 0, 0, 0}};
+    if (at < eights && row < (size_t)p.row_end) {
+      const u16x8* src = reinterpret_cast<const u16x8*>(p.x) + row * eights * (FROM == TOKENS8_SWIGLU ? 2 : 1) + at;
+      c.x = src[0];
+      if (FROM == TOKENS8_SWIGLU) c.up = src[eights];
+    }
+    return c;
+  };
+  // What is brought to 8 bits of them; what else is asked for of a SwiGLU is stored.
+  auto finish = [&](size_t row, const Columns& c, int q) {
+    if (FROM != TOKENS8_SWIGLU) return c.x;
+    const int at = lane + q * LANES;
+    const u16x8 h = swiglu8(c.x, c.up);
+    if (p.kept) {  // (a group's four lanes go together: lanes past the row have zeros)
+      const uint32_t eg = group_exponent(c.x), eu = group_exponent(c.up);
       if (at < eights) {
-        const u16x8* src = reinterpret_cast<const u16x8*>(p.x) + row * 2 * eights + at;
-        g = src[0];
-        u = src[eights];
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        held[q][k] = pack_bf16x2(swiglu_value(bf16_of(g, 2 * k), bf16_of(u, 2 * k)),
-                                 swiglu_value(bf16_of(g, 2 * k + 1), bf16_of(u, 2 * k + 1)));
-      if (p.kept) {  // (a group's four lanes go together: lanes past the row have zeros)
-        const uint32_t eg = group_exponent(g), eu = group_exponent(u);
-        if (at < eights) {
-          u8x8* codes = reinterpret_cast<u8x8*>(p.kept) + row * 2 * eights + at;
-          codes[0] = group_codes(g, eg);
-          codes[eights] = group_codes(u, eu);
-          if (at % 4 == 0) {
-            const size_t groups = keep8_groups(p.cols);
-            uint8_t* e = p.kept + keep8_exponents_at(2 * (size_t)p.rows, p.cols) + row * 2 * groups + at / 4;
-            e[0] = (uint8_t)eg;
-            e[groups] = (uint8_t)eu;
-          }
+        u8x8* codes = reinterpret_cast<u8x8*>(p.kept) + row * 2 * eights + at;
+        codes[0] = group_codes(c.x, eg);
+        codes[eights] = group_codes(c.up, eu);
+        if (at % 4 == 0) {
+          const size_t groups = keep8_groups(p.cols);
+          uint8_t* e = p.kept + keep8_exponents_at(2 * (size_t)p.rows, p.cols) + row * 2 * groups + at / 4;
+          e[0] = (uint8_t)eg;
+          e[groups] = (uint8_t)eu;
         }
       }
-      if (p.h && at < eights) reinterpret_cast<u16x8*>(p.h)[row * eights + at] = held[q];
-    } else if (at < eights) {
-      held[q] = reinterpret_cast<const u16x8*>(p.x)[row * eights + at];
     }
-    if (at < eights) {
-      float v[8];
-      values(held[q], at, v);
+    if (p.h && at < eights) reinterpret_cast<u16x8*>(p.h)[row * eights + at] = h;
+    return h;
+  };
+  uint32_t top = 0;
+  auto largest = [&](const u16x8& w, int q) {
+    if (lane + q * LANES >= eights) return;
+    float v[8];
+    values(w, q, v);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) top = max(top, magnitude(v[k]));
+    for (int k = 0; k < 8; ++k) top = max(top, magnitude(v[k]));
+  };
+
+  // A row's columns stay in registers, and the next row's are on their way while this one's codes are made.
+  [[maybe_unused]] int turn = 0;
+  const size_t step = (size_t)gridDim.x * (LANES == 64 ? 4 : 1);
+  size_t row = (size_t)p.row_begin + (LANES == 64 ? blockIdx.x * 4 + threadIdx.x / 64 : blockIdx.x);
+  Columns next[HOLD ? PIECES : 1];
+  u16x8 held[HOLD ? PIECES : 1];
+  if constexpr (HOLD)
+#pragma unroll
+    for (int q = 0; q < PIECES; ++q) next[q] = load(row, q);
+  for (; row < (size_t)p.row_end; row += step) {
+    top = 0;
+    if constexpr (HOLD) {
+#pragma unroll
+      for (int q = 0; q < PIECES; ++q) {
+        held[q] = finish(row, next[q], q);
+        largest(held[q], q);
+      }
+#pragma unroll
+      for (int q = 0; q < PIECES; ++q) next[q] = load(row + step, q);
+    } else {
+#pragma nounroll
+      for (int q = 0; q < PIECES; ++q) largest(finish(row, load(row, q), q), q);
     }
-  }
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
-  if constexpr (WAVES > 1) {
-    __shared__ uint32_t tops[WAVES];
-    if (threadIdx.x % 64 == 0) tops[threadIdx.x / 64] = top;
-    __syncthreads();
+    for (int d = 1; d < 64; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+    if constexpr (WAVES > 1) {
+      __shared__ uint32_t tops[2][WAVES];  // alternating: a wavefront may be a row ahead
+      uint32_t(&now)[WAVES] = tops[turn];
+      turn ^= 1;
+      if (threadIdx.x % 64 == 0) now[threadIdx.x / 64] = top;
+      __syncthreads();
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) top = max(top, tops[w]);
-  }
-  const RowScale r = row_scale_of(top);
-  if (lane == 0) p.scale[row] = r.s;
-#pragma unroll
-  for (int q = 0; q < PIECES; ++q) {
-    const int at = lane + q * LANES;
-    if (at < p.ld / 8) {  // (the columns up to a longer row's end are zeros)
+      for (int w = 0; w < WAVES; ++w) top = max(top, now[w]);
+    }
+    const RowScale r = row_scale_of(top);
+    if (lane == 0) p.scale[row] = r.s;
+    auto store = [&](const u16x8& w, int q) {
+      const int at = lane + q * LANES;
+      if (at >= p.ld / 8) return;  // (the columns up to a longer row's end are zeros)
       float v[8] = {};
-      if (at < eights) values(held[q], at, v);
+      if (at < eights) values(w, q, v);
       reinterpret_cast<u8x8*>(p.codes)[row * (p.ld / 8) + at] = row_codes(v, r);
+    };
+    if constexpr (HOLD) {
+#pragma unroll
+      for (int q = 0; q < PIECES; ++q) store(held[q], q);
+    } else {
+#pragma nounroll
+      for (int q = 0; q < PIECES; ++q) {
+        const Columns c = load(row, q);
+        store(FROM == TOKENS8_SWIGLU ? swiglu8(c.x, c.up) : c.x, q);
+      }
     }
   }
 }
@@ -100,7 +150,12 @@ hipError_t launch_tokens8(const Tokens8Args& args, hipStream_t st) {
   Tokens8Args a = args;
   auto go = [&](auto from_c) {
     constexpr int FROM = decltype(from_c)::value;
-    const unsigned blocks = (unsigned)((a.row_end - a.row_begin + plan.rows - 1) / plan.rows);
+    // Longer rows: as many blocks as the chip has room for at once, each with every so manyth row, the next on its way meanwhile (1531 rows of
+    // 13824 hidden activations: 27.8 us, with a block a row 30.6; 4096 of 11008 with factors 36.4 and 38.5).  Short plain ones: a block for each
+    // (4096 of 4096: 14.7, and 16.2 with 1024 blocks).
+    const size_t want = ((size_t)a.row_end - a.row_begin + plan.rows - 1) / plan.rows;
+    const size_t most = FROM == TOKENS8_PLAIN ? want : (FROM == TOKENS8_SCALED ? 768 : 512) * (size_t)(plan.pieces <= 2 ? 4 : 1);
+    const unsigned blocks = (unsigned)(want < most ? want : most);
     switch (plan.lanes * 100 + plan.pieces) {
       case 6401: tokens8_kernel<64, 1, FROM><<<blocks, 256, 0, st>>>(a); break;
       case 6402: tokens8_kernel<64, 2, FROM><<<blocks, 256, 0, st>>>(a); break;

@@ -1,4 +1,6 @@
 """Activations kept in 8 bits, and the backwards from them, against the definitions."""
+import ctypes
+
 import pytest
 import torch
 
@@ -61,7 +63,10 @@ def test_swiglu(gpu_api, shape):
     gu = ic.drawn_tokens(2, T, 2 * C)
     dh = ic.drawn_tokens(3, T, C)
     h, kept = gpu_api.swiglu_forward_keep8(gu.cuda(), C)
-    same(h, gpu_api.swiglu_forward_strided(gu.cuda(), C))
+    g64 = gu[:, :C].double()
+    h64 = g64 * torch.sigmoid(g64) * gu[:, C:].double()
+    tol = (8 + 4 * g64.abs()) * 2.0 ** -24 * h64.abs() + 1e-38
+    assert ((h.cpu().double() - h64).abs() <= tol + 2.0 ** -8 * (h64.abs() + tol)).all()
     same(gpu_api.restore8(kept, 2 * T, C), ic.restored8(gu.view(2 * T, C)))
     (q, s), kept2 = gpu_api.swiglu_forward_int8(gu.cuda(), C, keep=True)
     same(gpu_api.restore8(kept2, 2 * T, C), ic.restored8(gu.view(2 * T, C)))
@@ -71,6 +76,17 @@ def test_swiglu(gpu_api, shape):
     for got, ref in zip(gpu_api.swiglu_forward_int8(gu.cuda(), C, h=h3), (q, s)):
         same(got, ref)
     same(h3, h)
+    lib, P = gpu_api.load(), lambda t: ctypes.c_void_p(t.data_ptr())  # noqa: E731
+    for with_h in (True, False):                          # one output alone
+        h4, k4 = torch.empty_like(h), torch.empty_like(kept)
+        g = gu.cuda()
+        rc = lib.qalora_swiglu_forward8(T, C, P(g), P(h4) if with_h else None, None, None, None if with_h else P(k4), None)
+        torch.cuda.synchronize()
+        assert rc == gpu_api.OK
+        if with_h:
+            same(h4, h)
+        else:
+            same(gpu_api.restore8(k4, 2 * T, C), gpu_api.restore8(kept, 2 * T, C))
     dgu = gpu_api.swiglu_backward_kept8(dh.cuda(), kept, C).cpu()
     ref, tol = swiglu64(ic.restored8(gu.view(2 * T, C)).view(T, 2 * C), dh, C)
     bad = ((dgu.double() - ref).abs() > tol) | ~torch.isfinite(dgu)
