@@ -76,27 +76,20 @@ __device__ __forceinline__ void with_stages(int8_t* lds, int bytes, F&& f) {
 }
 }  // namespace
 
-// A block has BM tokens by BN columns, a wavefront TM x TN tiles of 16 x 16; the operand that runs down a result's registers is the
-// weight's, so that a lane has four neighbouring columns of a token.
+// BM tokens from m0 on by BN columns from n0 on, of WM x WN wavefronts; a wavefront has TM x TN tiles of 16 x 16, and the operand that runs
+// down a result's registers is the weight's, so that a lane has four neighbouring columns of a token.
 // ONCE: the weight is read by one row of tiles only, past the caches.
 template <bool BWD, int BM, int BN, int WM, int WN, int STAGES, bool ONCE>
-__global__ __launch_bounds__(WM* WN * 64) void gemm_i8_kernel(const Int8GemmArgs p) {
+__device__ __forceinline__ void gemm_i8_tile(const Int8GemmArgs& p, int8_t* lds, int m0, int n0) {
   constexpr int NT = WM * WN * 64, WAVES = WM * WN, POLICY = ONCE ? 2 : 0;  // 2: nontemporal
   constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
   constexpr int X_TILE = BM * I8_STEP, W_TILE = BN * I8_STEP, STAGE = X_TILE + W_TILE;
   constexpr int X_LOADS = X_TILE / 16 / NT, W_LOADS = W_TILE / 16 / NT;  // sixteen bytes each, of a thread
   static_assert(X_LOADS * NT * 16 == X_TILE && W_LOADS * NT * 16 == W_TILE, "whole loads");
-  extern __shared__ __align__(1024) int8_t lds[];
-
+  static_assert(!BWD || (BN / 16 & (BN / 16 - 1)) == 0, "places by exclusive or");
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave % WM, wn = wave / WM;
-  const int tiles_m = ceil_div(p.M, BM), tiles_n = ceil_div(p.N, BN);
-  const int tile = xcd_run(blockIdx.x, tiles_m * tiles_n);
-  constexpr int BAND = 4;  // row tiles that are walked together across the columns
-  const int band = tile / (BAND * tiles_n), in_band = tile - band * BAND * tiles_n;
-  const int band_rows = min(BAND, tiles_m - band * BAND);
-  const int m0 = (band * BAND + in_band % band_rows) * BM, n0 = (in_band / band_rows) * BN;
   // blockIdx.y: which slice of K (its sums are added up by a later launch)
   const int all = ceil_div(p.K, I8_STEP), per = ceil_div(all, (int)gridDim.y);
   const int begin = blockIdx.y * per, steps = min(all, begin + per) - begin;
@@ -304,7 +297,7 @@ __global__ __launch_bounds__(WM* WN * 64) void gemm_i8_kernel(const Int8GemmArgs
     bias[1] = reinterpret_cast<const f32x4*>(p.epi.bias + col)[1];
   }
   // The other operands of a thread's next rows are asked for while the rows before are finished.
-  constexpr int ROWS = ceil_div(PB * 16, ROWS_AT_ONCE), BATCH = ROWS % 4 == 0 ? 4 : ROWS % 3 == 0 ? 3 : ROWS % 2 == 0 ? 2 : 1;
+  constexpr int ROWS = ceil_div(PB * 16, ROWS_AT_ONCE), BATCH = ROWS < 4 ? ROWS : 4, ROUND = ceil_div(ROWS, BATCH) * BATCH;
   // (a thread's rows of a pass; how many are on their way)
   EpilogueOperands coming[BATCH];
   auto ask = [&](int pass, int row, EpilogueOperands& o) {
@@ -335,7 +328,7 @@ __global__ __launch_bounds__(WM* WN * 64) void gemm_i8_kernel(const Int8GemmArgs
         const EpilogueOperands now = coming[k];
         const int next = first + k + BATCH;
         if (next < ROWS) ask(pass, next, coming[k]);
-        else if (pass + 1 < TM / PB) ask(pass + 1, next - ROWS, coming[k]);
+        else if (next >= ROUND && pass + 1 < TM / PB) ask(pass + 1, next - ROUND, coming[k]);
         const int rl = row_in + (first + k) * ROWS_AT_ONCE;
         if (!col_ok || rl >= PB * 16 || base + rl >= p.M) continue;
         const char* src = stage_lds + rl * CW * 4;
@@ -355,6 +348,37 @@ __global__ __launch_bounds__(WM* WN * 64) void gemm_i8_kernel(const Int8GemmArgs
       }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the pass has been read out
+  }
+}
+
+// Tile t of tiles_m x tiles_n: rows of tiles are walked in bands of four across the columns.
+__device__ __forceinline__ int2 tile_place(int t, int tiles_m, int tiles_n) {
+  constexpr int BAND = 4;
+  const int band = t / (BAND * tiles_n), in_band = t - band * BAND * tiles_n, rows = min(BAND, tiles_m - band * BAND);
+  return int2{band * BAND + in_band % rows, in_band / rows};
+}
+template <bool BWD, int BM, int BN, int WM, int WN, int STAGES, bool ONCE>
+__global__ __launch_bounds__(WM* WN * 64) void gemm_i8_kernel(const Int8GemmArgs p) {
+  extern __shared__ __align__(1024) int8_t lds[];
+  const int tiles_m = ceil_div(p.M, BM), tiles_n = ceil_div(p.N, BN);
+  const int2 at = tile_place(xcd_run(blockIdx.x, tiles_m * tiles_n), tiles_m, tiles_n);
+  gemm_i8_tile<BWD, BM, BN, WM, WN, STAGES, ONCE>(p, lds, at.x * BM, at.y * BN);
+}
+// 256 x 256 tiles of the first columns and 256 x NARROW ones of the rest: see int8_narrow.  Half of the narrow ones come first: the
+// compute units that get them are then out of step with the others, and do not all come to the ends of their tiles, where only memory
+// works, at the same time.
+template <bool BWD, int NARROW>
+__global__ __launch_bounds__(512) void gemm_i8_mixed_kernel(const Int8GemmArgs p, int wide_n) {
+  extern __shared__ __align__(1024) int8_t lds[];
+  const int tiles_m = ceil_div(p.M, 256), narrow_n = ceil_div(p.N - wide_n * 256, NARROW);
+  const int wide = tiles_m * wide_n, narrow = tiles_m * narrow_n, first = int8_narrow_first(narrow), b = blockIdx.x;
+  if (b >= first && b < first + wide) {
+    const int2 at = tile_place(xcd_run(b - first, wide), tiles_m, wide_n);
+    gemm_i8_tile<BWD, 256, 256, 2, 4, 2, false>(p, lds, at.x * 256, at.y * 256);
+  } else {
+    const int t = b < first ? xcd_run(b, first) : first + xcd_run(b - first - wide, narrow - first);
+    const int2 at = tile_place(t, tiles_m, narrow_n);
+    gemm_i8_tile<BWD, 256, NARROW, 4, 2, 2, false>(p, lds, at.x * 256, wide_n * 256 + at.y * NARROW);
   }
 }
 
@@ -398,11 +422,27 @@ static hipError_t launch_tile(const Int8GemmArgs& a, int slices, hipStream_t st)
 
 // Forward, a weight that one row of tiles reads goes past the caches (16 x 22016 x 8192: 36.7 us, 40.8 through them; 61 x 13824 x 5120: 20
 // and 21.2); backward, where a tile's rows of the weight are parts of lines, that gains nothing.
+template <bool BWD, int NARROW>
+static hipError_t launch_mixed(const Int8GemmArgs& a, int wide_n, hipStream_t st) {
+  auto kernel = gemm_i8_mixed_kernel<BWD, NARROW>;
+  constexpr int bytes = 2 * 512 * I8_STEP;
+  static std::atomic<uint64_t> granted{0};  // per instantiation
+  if (hipError_t e = grant_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes, granted); e != hipSuccess) return e;
+  const int tiles_m = ceil_div(a.M, 256);
+  kernel<<<(unsigned)(tiles_m * (wide_n + ceil_div(a.N - wide_n * 256, NARROW))), 512, bytes, st>>>(a, wide_n);
+  return hipGetLastError();
+}
+
 template <bool BWD>
 static hipError_t launch_planned(const Int8GemmArgs& a, const Int8Plan& plan, hipStream_t st) {
   const int s = plan.slices;
   switch (plan.tile) {
-    case I8_256x256: return launch_tile<BWD, 256, 256, 2, 4, 2>(a, s, st);
+    case I8_256x256:
+      if (const Int8Mixed m = int8_mixed(a.M, a.N, s, BWD); m.narrow == 128) return launch_mixed<BWD, 128>(a, m.wide_n, st);
+      else if constexpr (!BWD) {
+        if (m.narrow == 192) return launch_mixed<false, 192>(a, m.wide_n, st);
+      }
+      return launch_tile<BWD, 256, 256, 2, 4, 2>(a, s, st);
     case I8_192x256: return launch_tile<BWD, 192, 256, 2, 4, 2>(a, s, st);
     case I8_128x256: return launch_tile<BWD, 128, 256, 2, 4, 3>(a, s, st);
     case I8_128x128: return launch_tile<BWD, 128, 128, 4, 2, 2>(a, s, st);

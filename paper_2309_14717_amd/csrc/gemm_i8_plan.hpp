@@ -1,5 +1,6 @@
 // Which tile a product of 8-bit integers takes, and into how many slices its K is split (gemm_i8.hip).
 #pragma once
+#include <hip/hip_runtime.h>
 #include <stddef.h>
 
 namespace qalora {
@@ -62,6 +63,20 @@ inline Int8Plan int8_plan(int M, int N, int K, bool back) {
     }
   }
   return best;
+}
+// A product of some rounds of 256 x 256 tiles and part of another: the columns of whole rounds keep them, and the others' tiles are as narrow
+// as leaves them one round.  narrow = 0: all tiles alike.
+struct Int8Mixed {
+  int narrow, wide_n;
+};
+__host__ __device__ inline int int8_narrow_first(int narrow) { return narrow / 2 / 8 * 8; }
+inline Int8Mixed int8_mixed(int M, int N, int slices, bool back) {
+  const long tiles_m = ((long)M + 255) / 256, tiles = tiles_m * ((N + 255) / 256), rounds = tiles / 256;
+  if (slices > 1 || rounds < 1 || tiles % 256 == 0 || tiles_m > 256) return Int8Mixed{0, 0};
+  const int wide_n = (int)(rounds * 256 / tiles_m), rest = N - wide_n * 256;
+  for (const int w : {128, 192})
+    if (!(back && w == 192) && tiles_m * ((rest + w - 1) / w) <= 256) return Int8Mixed{w, wide_n};
+  return Int8Mixed{0, 0};
 }
 // Room for the slices' sums of any number of tokens up to M.
 inline size_t int8_partials(int M, int N) {
