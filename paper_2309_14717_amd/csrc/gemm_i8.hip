@@ -364,7 +364,7 @@ __global__ __launch_bounds__(WM* WN * 64) void gemm_i8_kernel(const Int8GemmArgs
   const int2 at = tile_place(xcd_run(blockIdx.x, tiles_m * tiles_n), tiles_m, tiles_n);
   gemm_i8_tile<BWD, BM, BN, WM, WN, STAGES, ONCE>(p, lds, at.x * BM, at.y * BN);
 }
-// 256 x 256 tiles of the first columns and 256 x NARROW ones of the rest: see int8_narrow.  Half of the narrow ones come first: the
+// 256 x 256 tiles of the first columns and 256 x NARROW ones of the rest: see int8_mixed.  Half of the narrow ones come first: the
 // compute units that get them are then out of step with the others, and do not all come to the ends of their tiles, where only memory
 // works, at the same time.
 template <bool BWD, int NARROW>

@@ -12,6 +12,8 @@ SHAPES = [(1, 16, 8), (1, 4096, 1032), (3, 1024, 264), (4, 11008, 520), (7, 48, 
 BACK_SHAPES = [(5, 64, 11008), (300, 16, 4104)]
 # tokens, depth and width of the product, for the larger tiles
 LARGE = [(700, 64, 16400), (500, 144, 16400), (380, 64, 11024), (380, 272, 8208), (250, 144, 4112), (140, 272, 16400), (513, 80, 8208)]
+# the same, of more than a round of 256 x 256 tiles: the last columns in tiles of 256 x 128 and 256 x 192
+MIXED = [(65000, 16, 272), (64800, 144, 336), (2040, 144, 19408), (4090, 144, 6704), (8200, 144, 3024), (700, 80, 32784)]
 
 
 def rows8(v):

@@ -180,7 +180,7 @@ def test_gradient_is_the_forwards_difference(gpu_api, shape):
     assert float((dy.double() * (y(x + d) - y(x - d))).sum()) == 2 * float((dx * d.double()).sum())
 
 
-@pytest.mark.parametrize("size", ic.LARGE, ids=str)
+@pytest.mark.parametrize("size", ic.LARGE + ic.MIXED, ids=str)
 def test_large_tiles(gpu_api, size):
     """Both directions of a product, with an epilogue, against 64 bits on the GPU."""
     T, depth, width = size

@@ -22,6 +22,14 @@ extern "C" void product(int M, int N, int K, int back, int* o) {
   const Int8Plan p = int8_plan(M, N, K, back);
   o[0] = p.tile; o[1] = p.slices; o[2] = kInt8Tiles[p.tile].rows; o[3] = kInt8Tiles[p.tile].cols; o[4] = kInt8Tiles[p.tile].threads;
 }
+extern "C" void mixed(int M, int N, int slices, int back, int* o) {
+  const Int8Mixed m = int8_mixed(M, N, slices, back);
+  o[0] = m.narrow; o[1] = m.wide_n;
+  if (m.narrow) {
+    const int tiles_m = (M + 255) / 256, narrow = tiles_m * ((N - m.wide_n * 256 + m.narrow - 1) / m.narrow);
+    o[2] = tiles_m * m.wide_n; o[3] = narrow; o[4] = int8_narrow_first(narrow);
+  }
+}
 extern "C" long long partials(int M, int N) { return (long long)int8_partials(M, N); }
 extern "C" long long kept(long long rows, long long cols) { return (long long)keep8_bytes(rows, cols); }
 extern "C" long long exponents_at(long long rows, long long cols) { return (long long)keep8_exponents_at(rows, cols); }
@@ -74,6 +82,33 @@ def test_product_plans(host):
             host.product(T, width, depth, back, o)
             got.add((o[0], o[1] > 1))
         assert {t for t, _ in got} == set(range(11)) - ({4, 6, 8, 10} if back else {7, 9}), (back, sorted(got))
+
+
+def test_mixed_plans(host):
+    """Whole rounds of wide tiles, the rest in one round of narrow ones, every column in one of them; the GPU tests reach each kind."""
+    o, m = (ctypes.c_int * 5)(), (ctypes.c_int * 5)()
+    rng = random.Random(4)
+    seen = set()
+    for M, N in [(1, 131072), (65536, 8), (65537, 8), (2 ** 29, 131072), (65536, 256), (65536, 264), (4096, 4096), (4096, 4104)] + \
+                [(rng.randint(1, 10 ** rng.randint(3, 6)), 8 * rng.randint(1, 16384)) for _ in range(4000)]:
+        for back in (0, 1):
+            host.mixed(M, N, 2, back, m)
+            assert m[0] == 0
+            host.mixed(M, N, 1, back, m)
+            narrow, wide_n, wide, narrows, first = m
+            seen.add((back, narrow))
+            tiles = -(-M // 256) * -(-N // 256)
+            if narrow:
+                assert wide_n > 0 and 0 < N - 256 * wide_n and 256 * (tiles // 256) - -(-M // 256) < wide <= 256 * (tiles // 256)
+                assert 0 <= first <= narrows <= 256 and first % 8 == 0 and (wide + narrows) * 512 < 2 ** 32
+    assert seen == {(0, 0), (0, 128), (0, 192), (1, 0), (1, 128)}
+    for back in (0, 1):
+        got = set()
+        for T, depth, width in ic.MIXED:
+            host.product(T, width, depth, back, o)
+            host.mixed(T, width, o[1], back, m)
+            got.add((o[0], m[0]))
+        assert got == ({(0, 0), (0, 128)} if back else {(0, 128), (0, 192)})
 
 
 def test_kept_sizes(host):
