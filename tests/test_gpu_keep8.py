@@ -93,6 +93,19 @@ def test_swiglu(gpu_api, shape):
     assert not bad.any(), (int(bad.sum()), bad.nonzero()[0].tolist())
 
 
+@pytest.mark.parametrize("C", [40, 1024, 5128, 22016])
+def test_swiglu_of_infinities_and_nan(gpu_api, C):
+    """A row whose hidden activations are not all finite has a NaN scale and codes of zero; its kept groups that are finite stay."""
+    gu = ic.drawn_tokens(6, 7, 2 * C)
+    gu[1, 3], gu[2, C + 5], gu[4, C - 1], gu[5, 2 * C - 1] = float("inf"), float("nan"), float("-inf"), float("-inf")
+    (q, s), kept = gpu_api.swiglu_forward_int8(gu.cuda(), C, keep=True)
+    h = gpu_api.swiglu_forward_keep8(gu.cuda(), C)[0].cpu()
+    assert (torch.isfinite(h).all(1) == torch.tensor([True, False, False, True, False, False, True])).all()
+    for got, ref in zip((q, s), ic.rows8(h.float())):
+        same(got, ref.to(got.dtype))
+    same(gpu_api.restore8(kept, 14, C), ic.restored8(gu.view(14, C)))
+
+
 def test_swiglu_gradient_against_differences(gpu_api):
     """Gate and up on the kept grid; differences of the definition in 64 bits."""
     T, C = 6, 96
