@@ -123,9 +123,10 @@ __device__ __forceinline__ void gemm_i8_tile(const Int8GemmArgs& p, int8_t* lds,
   auto request = [&](int it, int8_t* to) {
     const int k0 = (begin + it) * I8_STEP;
     const uint32_t dead = k0 + 16 * chunk8 < k_end ? 0u : kPast;  // (past the last step too: as many loads whatever the step)
+    const int from = k0 < k_end ? k0 : 0;                         // (a scalar offset past the operand's end has no meaning)
 #pragma unroll
     for (int q = 0; q < X_LOADS; ++q)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_x, (lds_void*)(to + (q * WAVES + wave) * 1024), 16, (int)(x_off[q] | dead), k0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_x, (lds_void*)(to + (q * WAVES + wave) * 1024), 16, (int)(x_off[q] | dead), from, 0, 0);
     if (BWD) {
       const int rows = max(0, min(I8_STEP, k_end - k0));
       const uint32_t bytes = rows > 0 ? (uint32_t)rows * (uint32_t)p.N - (uint32_t)n0 : 0u;
@@ -137,7 +138,7 @@ __device__ __forceinline__ void gemm_i8_tile(const Int8GemmArgs& p, int8_t* lds,
       const __amdgpu_buffer_rsrc_t rs_w = tile_rsrc(w_base, w_rows * (uint32_t)p.K);
 #pragma unroll
       for (int q = 0; q < W_LOADS; ++q)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_w, (lds_void*)(to + X_TILE + (q * WAVES + wave) * 1024), 16, (int)(w_off[q] | dead), k0, 0, POLICY);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_w, (lds_void*)(to + X_TILE + (q * WAVES + wave) * 1024), 16, (int)(w_off[q] | dead), from, 0, POLICY);
     }
   };
 
@@ -420,8 +421,6 @@ static hipError_t launch_tile(const Int8GemmArgs& a, int slices, hipStream_t st)
   return hipGetLastError();
 }
 
-// Forward, a weight that one row of tiles reads goes past the caches (16 x 22016 x 8192: 36.7 us, 40.8 through them; 61 x 13824 x 5120: 20
-// and 21.2); backward, where a tile's rows of the weight are parts of lines, that gains nothing.
 template <bool BWD, int NARROW>
 static hipError_t launch_mixed(const Int8GemmArgs& a, int wide_n, hipStream_t st) {
   auto kernel = gemm_i8_mixed_kernel<BWD, NARROW>;
@@ -433,6 +432,8 @@ static hipError_t launch_mixed(const Int8GemmArgs& a, int wide_n, hipStream_t st
   return hipGetLastError();
 }
 
+// Forward, a weight that one row of tiles reads goes past the caches (16 x 22016 x 8192: 36.7 us, 40.8 through them; 61 x 13824 x 5120: 20
+// and 21.2); backward, where a tile's rows of the weight are parts of lines, that gains nothing.
 template <bool BWD>
 static hipError_t launch_planned(const Int8GemmArgs& a, const Int8Plan& plan, hipStream_t st) {
   const int s = plan.slices;
