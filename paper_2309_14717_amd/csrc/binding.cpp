@@ -763,7 +763,7 @@ PyObject* epilogue_backward_of(PyObject* const* a, bool kept8) {
     PLAIN(c);
     ws = *t;
   } else if (dbias.defined()) {
-    ws = c.scratch(Py_None, lib.qalora_epilogue_backward_workspace_bytes((int)T, (int)cols));
+    if (const size_t n = lib.qalora_epilogue_backward_workspace_bytes((int)T, (int)cols)) ws = c.scratch(Py_None, n);
   }
   PLAIN(c);
   auto data = [](const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; };
