@@ -1,6 +1,8 @@
 // Values in 8 bits, device side: codes of rows with one scale each (tokens, weight channels), and of groups of 32 columns
 // that share an exponent (kept activations).
 #pragma once
+#include <type_traits>
+
 #include "common.hpp"
 #include "epilogue.hpp"
 
@@ -40,38 +42,53 @@ struct RowScale {
   float s;    // as stored: NaN for a row with an infinity or a NaN, then all codes are 0
   float up;   // v and s times this power of two are ordinary numbers whatever the row's magnitude
   float by;   // s * up
-  float inv;  // 1 / by, 0 for a row without a scale
+  float inv;  // 1 / by (to 2^-24 (1 + 2^-20) of it), 0 for a row without a scale
 };
 // `top`: the bits of the row's largest magnitude (as integers those of finite values, infinities and NaNs come in that order)
 __device__ __forceinline__ RowScale row_scale_of(uint32_t top) {
   RowScale r;
   const bool finite = top < 0x7f800000u;
-  const float s = finite ? __uint_as_float(top) / 127.0f : __uint_as_float(0x7fc00000u);
-  r.s = s;
+  // A quotient by a constant: an estimate, its remainder (exact), and one correction give the nearest number (Markstein), but among numbers
+  // so small that the remainder is none any more.
+  const float m = __uint_as_float(top), by127 = 1.0f / 127.0f, estimate = m * by127;
+  float s = __builtin_fmaf(__builtin_fmaf(-estimate, 127.0f, m), by127, estimate);
+  if (top < 0x0d000000u) s = m / 127.0f;  // (below 2^-101)
+  r.s = finite ? s : __uint_as_float(0x7fc00000u);
   r.up = top < 0x20000000u ? 0x1p64f : 1.0f;  // below 2^-63
   r.by = finite ? s * r.up : 0.0f;
-  r.inv = r.by > 0.0f ? 1.0f / r.by : 0.0f;
+  const float guess = __builtin_amdgcn_rcpf(r.by), inv = __builtin_fmaf(__builtin_fmaf(-r.by, guess, 1.0f), guess, guess);
+  r.inv = r.by > 0.0f ? inv : 0.0f;
   return r;
 }
-// The codes of eight v.  v inv is off by at most 127 2^-23 = 1.6e-5 from the quotient, so rounding it can go wrong only that close to the
-// middle between two codes; there the remainder v - code s, which fp32 holds exactly (it is a multiple of the smaller of the last
-// places of v and s, and at most about s / 2), says which side v is on.  (A quotient is past 127 only where s is subnormal.)
+// The largest of a wavefront's words, the same in every lane.
+__device__ __forceinline__ uint32_t wave_top(uint32_t v) {
+  auto with = [&](auto control) { v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, decltype(control)::value, 0xf, 0xf, true)); };
+  with(std::integral_constant<int, 0xb1>{});   // the neighbour
+  with(std::integral_constant<int, 0x4e>{});   // the other pair of four
+  with(std::integral_constant<int, 0x141>{});  // half a row of sixteen, mirrored
+  with(std::integral_constant<int, 0x140>{});  // the row, mirrored
+  uint32_t rows[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) rows[k] = (uint32_t)__builtin_amdgcn_readlane((int)v, 16 * k);
+  return max(max(rows[0], rows[1]), max(rows[2], rows[3]));
+}
+// The codes of eight v.  inv is a last place from 1 / by at most, so v inv is off by at most 127 2^-24 (1 + 2^-20) = 7.6e-6 from the quotient, and
+// rounding it can go wrong only that close to the middle between two codes; there the remainder v - code s, which fp32 holds exactly (it
+// is a multiple of the smaller of the last places of v and s, and at most about s / 2), says which side v is on.  (A quotient is past
+// 127 only where s is subnormal.)
 __device__ __forceinline__ float exact_code(float v, float t, const RowScale& r) {
-  float q = __builtin_rintf(t);
-  const float left = __builtin_fmaf(-q, r.by, v), twice = __builtin_fabsf(left) + __builtin_fabsf(left);
-  const bool odd = ((int)q & 1) != 0;
-  if (twice > r.by || (twice == r.by && odd)) q += left > 0.0f ? 1.0f : -1.0f;
-  return __builtin_amdgcn_fmed3f(q, -127.0f, 127.0f) + kWhole;
+  const float q = __builtin_rintf(t), left = __builtin_fmaf(-q, r.by, v), twice = __builtin_fabsf(left) + __builtin_fabsf(left);
+  const bool past = (twice > r.by) | ((twice == r.by) & (((int)q & 1) != 0));
+  return __builtin_amdgcn_fmed3f(q + (past ? __builtin_copysignf(1.0f, left) : 0.0f), -127.0f, 127.0f) + kWhole;
 }
 __device__ __forceinline__ u8x8 row_codes(const float (&v)[8], const RowScale& r) {
-  float t[8], f[8], worst = 0.0f;
+  float f[8], worst = 0.0f;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    t[k] = v[k] * r.inv;
-    f[k] = t[k] + kWhole;  // the code in its low byte
-    worst = fmaxf(worst, __builtin_fabsf(t[k] - (f[k] - kWhole)));
+    f[k] = __builtin_fmaf(v[k], r.inv, kWhole);  // the code in its low byte
+    worst = fmaxf(worst, __builtin_fabsf(__builtin_fmaf(v[k], r.inv, kWhole - f[k])));
   }
-  if (worst > 0.49995f || r.up != 1.0f) {
+  if (worst > 0.49999f || r.up != 1.0f) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const float w = v[k] * r.up;

@@ -62,8 +62,7 @@ __global__ __launch_bounds__(S8_WAVES * 64, 4) void stream_i8_kernel(const Strea
 #pragma unroll
       for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(bf16_of(w, k)) & 0x7fffffffu);
     }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+    top = wave_top(top);
     if (lane == 0) tops[wave % share][t] = top;
   }
   __syncthreads();

@@ -2,7 +2,10 @@
 // and the channels of a weight.
 //   s = fl32(max |v| / 127),   code = rne(v / s)
 // The tokens' kernel reads a row once: a block (or a wavefront, for rows up to 1024 columns) has it whole in registers as bf16 when the
-// largest magnitude is known.  Bound by its bytes, 3 a column (SwiGLU: 5, and 2 more with the kept halves).
+// largest magnitude is known.  Bound by its bytes, 3 a column (SwiGLU: 5, and 2 more with the kept halves), and nearly as much by its
+// arithmetic, eleven operations a column: 4096 rows of 11008 with factors 30 us, 4.5 TB/s (with a quotient's exactness looked at by 13
+// operations 36 us), 4096 plain ones of 4096 14.2 us, 1531 rows of 13824 hidden activations 25 us; without the codes' arithmetic
+// the last two take 11.3 and 22.
 #include "int8.hpp"
 #include "kernels.hpp"
 #include "tokens8_plan.hpp"
@@ -112,8 +115,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void tokens8_kernel(cons
 #pragma nounroll
       for (int q = 0; q < PIECES; ++q) largest(finish(row, load(row, q), q), q);
     }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+    top = wave_top(top);
     if constexpr (WAVES > 1) {
       __shared__ uint32_t tops[2][WAVES];  // alternating: a wavefront may be a row ahead
       uint32_t(&now)[WAVES] = tops[turn];
@@ -150,22 +152,17 @@ hipError_t launch_tokens8(const Tokens8Args& args, hipStream_t st) {
   Tokens8Args a = args;
   auto go = [&](auto from_c) {
     constexpr int FROM = decltype(from_c)::value;
-    // Longer rows: as many blocks as the chip has room for at once, each with every so manyth row, the next on its way meanwhile (1531 rows of
-    // 13824 hidden activations: 27.8 us, with a block a row 30.6; 4096 of 11008 with factors 36.4 and 38.5).  Short plain ones: a block for each
-    // (4096 of 4096: 14.7, and 16.2 with 1024 blocks).
     const size_t want = ((size_t)a.row_end - a.row_begin + plan.rows - 1) / plan.rows;
-    const size_t most = FROM == TOKENS8_PLAIN ? want : (FROM == TOKENS8_SCALED ? 768 : 512) * (size_t)(plan.pieces <= 2 ? 4 : 1);
+    const size_t most = tokens8_blocks(plan, a.rows, FROM == TOKENS8_PLAIN, FROM == TOKENS8_SWIGLU);
     const unsigned blocks = (unsigned)(want < most ? want : most);
     switch (plan.lanes * 100 + plan.pieces) {
       case 6401: tokens8_kernel<64, 1, FROM><<<blocks, 256, 0, st>>>(a); break;
       case 6402: tokens8_kernel<64, 2, FROM><<<blocks, 256, 0, st>>>(a); break;
       case 25601: tokens8_kernel<256, 1, FROM><<<blocks, 256, 0, st>>>(a); break;
       case 25602: tokens8_kernel<256, 2, FROM><<<blocks, 256, 0, st>>>(a); break;
-      case 25603: tokens8_kernel<256, 3, FROM><<<blocks, 256, 0, st>>>(a); break;
-      case 25604: tokens8_kernel<256, 4, FROM><<<blocks, 256, 0, st>>>(a); break;
-      case 25606: tokens8_kernel<256, 6, FROM><<<blocks, 256, 0, st>>>(a); break;
-      case 25608: tokens8_kernel<256, 8, FROM><<<blocks, 256, 0, st>>>(a); break;
-      case 25612: tokens8_kernel<256, 12, FROM><<<blocks, 256, 0, st>>>(a); break;
+      case 51202: tokens8_kernel<512, 2, FROM><<<blocks, 512, 0, st>>>(a); break;
+      case 51203: tokens8_kernel<512, 3, FROM><<<blocks, 512, 0, st>>>(a); break;
+      case 51204: tokens8_kernel<512, 4, FROM><<<blocks, 512, 0, st>>>(a); break;
       case 102401: tokens8_kernel<1024, 1, FROM><<<blocks, 1024, 0, st>>>(a); break;
       case 102402: tokens8_kernel<1024, 2, FROM><<<blocks, 1024, 0, st>>>(a); break;
       case 102404: tokens8_kernel<1024, 4, FROM><<<blocks, 1024, 0, st>>>(a); break;
