@@ -3,6 +3,9 @@
 //   backward  dx[t, i] = s[t] sum_j q[t, j] w8[j, i]            K = d_out (the channels' scales are in q)
 // and the epilogue on that.  One copy of the weight's codes, [d_out, d_in], serves both directions: the forward's operands lie along K in
 // it, the backward's are turned by transposing LDS reads.
+// Large products are bound by the matrix instructions and the chip's power: 4096 tokens, K = 11008, 4096 columns, either direction 147 us,
+// 2500 TOP/s.  A step of K is 128, whole cache lines of every row (64: 216 us for 4096 x 11008 x 4096 that take 180); the backward's reads
+// wait in a block of their own (by the builtin, before which all loads on their way are waited for: 183 us).
 #include <atomic>
 #include <type_traits>
 
@@ -367,7 +370,7 @@ __global__ __launch_bounds__(WM* WN * 64) void gemm_i8_kernel(const Int8GemmArgs
 }
 // 256 x 256 tiles of the first columns and 256 x NARROW ones of the rest: see int8_mixed.  Half of the narrow ones come first: the
 // compute units that get them are then out of step with the others, and do not all come to the ends of their tiles, where only memory
-// works, at the same time.
+// works, at the same time (4096 x 11008 x 4096 with silu, product and z: 219 us, and 227 with all tiles alike; without 180 and 183 to 210).
 template <bool BWD, int NARROW>
 __global__ __launch_bounds__(512) void gemm_i8_mixed_kernel(const Int8GemmArgs p, int wide_n) {
   extern __shared__ __align__(1024) int8_t lds[];

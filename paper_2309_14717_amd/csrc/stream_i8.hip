@@ -2,7 +2,8 @@
 // its first weights are on their way, and the weight is read once, straight into registers.
 //   z[t, j] = s[t] sw[j] sum_i q[t, i] w8[j, i]
 // A block has sixteen output channels and all tokens; its wavefronts share K, every eighth 128 bytes of the rows each, so that a
-// channel's sum needs no other block.
+// channel's sum needs no other block.  Bound by the weight's bytes: 1 x 22016 x 8192 33 us, 5.4 TB/s (more loads ahead, or fewer registers for
+// another block a compute unit: no faster); 16 x 1024 x 1024 6 us, of which the tokens' codes are 2.5.
 #include "int8.hpp"
 #include "epilogue.hpp"
 #include "kernels.hpp"
