@@ -300,7 +300,8 @@ int qalora_epilogue_backward(int act, int tokens, int cols, const void* dy, int 
  * codes int8 [d_out, d_in], scale fp32 [d_out]: one copy serves both directions.  d_in a multiple of 16, d_out a multiple of 8, both at
  * most QALORA_INT8_MAX_SIDE (the sums then fit 32 bits), tokens of a product at most 2^29;
  * QALORA_EUNSUPPORTED otherwise.  Operands may pass 4 GB.
- * All of these may be captured into a HIP graph after one eager call of the same shape; reruns are bit-identical. */
+ * All of these may be captured into a HIP graph after one eager call of the same shape; reruns are bit-identical, and a token's results
+ * are the same bit for bit whatever other tokens, and however many, are with it. */
 #define QALORA_INT8_MAX_SIDE 131072
 /* W fp32 [d_in, d_out] (row-major, as everywhere) -> codes [d_out, d_in], scale [d_out]. */
 int qalora_quantize_int8(int d_in, int d_out, const float* W, int8_t* codes, float* scale, void* stream);

@@ -317,10 +317,7 @@ __device__ __forceinline__ void gemm_i8_tile(const Int8GemmArgs& p, int8_t* lds,
       const int b = pass * PB + k;
 #pragma unroll
       for (int a = 0; a < TN; ++a) {
-        f32x4 v;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = (float)acc[a][b][r] * sc[b] * by[a][r];
-        *reinterpret_cast<f32x4*>(stage_lds + (k * 16 + fr) * CW * 4 + (((4 * a + fc) ^ (fr & MASK)) << 4)) = v;
+        *reinterpret_cast<f32x4*>(stage_lds + (k * 16 + fr) * CW * 4 + (((4 * a + fc) ^ (fr & MASK)) << 4)) = scaled_sums(acc[a][b], sc[b], by[a]);
       }
     }
     const int base = m0 + (wm * TM + pass * PB) * 16;
@@ -402,11 +399,9 @@ __global__ __launch_bounds__(256) void gemm_i8_sum_kernel(const Int8GemmArgs p, 
     for (; s < slices; ++s) acc += *reinterpret_cast<const i32x4*>(p.partial + s * n + at);
     const int m = (int)(at / p.N), col = (int)(at % p.N);
     const float sc = p.row_scale[m];
-    f32x4 by = {1.0f, 1.0f, 1.0f, 1.0f}, v;
+    f32x4 by = {1.0f, 1.0f, 1.0f, 1.0f};
     if (p.col_scale) by = *reinterpret_cast<const f32x4*>(p.col_scale + col);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = (float)acc[r] * sc * by[r];
-    v = apply_epilogue(p.epi, v, at, col, p.out_bf16);
+    const f32x4 v = apply_epilogue(p.epi, scaled_sums(acc, sc, by), at, col, p.out_bf16);
     if (p.out_bf16)
       *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at) = uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
     else

@@ -102,6 +102,17 @@ __device__ __forceinline__ u8x8 row_codes(const float (&v)[8], const RowScale& r
   return u8x8{low_bytes(c[0], c[1], c[2], c[3]) & mask, low_bytes(c[4], c[5], c[6], c[7]) & mask};
 }
 
+// (acc s) by of four columns, each product rounded: not joined with a bias or a residual that is added next, so that a token's results do not
+// depend on the kernel that the number of tokens chooses.
+template <typename Sums>
+__device__ __forceinline__ f32x4 scaled_sums(const Sums& acc, float s, const f32x4& by) {
+#pragma clang fp contract(off)
+  f32x4 v;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) v[r] = (float)acc[r] * s * by[r];
+  return v;
+}
+
 // ---- 32 neighbouring columns share an exponent ---------------------------------------------------------------------------
 
 constexpr int kKeepGroup = 32;  // columns: four lanes of eight

@@ -115,10 +115,7 @@ __global__ __launch_bounds__(S8_WAVES * 64, 4) void stream_i8_kernel(const Strea
 #pragma unroll
   for (int w = 1; w < S8_WAVES; ++w) acc += *reinterpret_cast<const i32x4*>(sums[w][lane]);
   const float s = scales[fr];
-  f32x4 v;
-#pragma unroll
-  for (int r = 0; r < 4; ++r) v[r] = (float)acc[r] * s * by[r];
-  v = apply_four(p.epi, operands, v, at);
+  const f32x4 v = apply_four(p.epi, operands, scaled_sums(acc, s, by), at);
   if (p.out_bf16)
     *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at) = uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
   else

@@ -286,6 +286,51 @@ def test_a_row_that_is_nan_stays_alone(gpu_api, T):
     same(dx[rows], gpu_api.backward_int8(dy, *w)[rows])
 
 
+@pytest.mark.parametrize("size", [(1024, 1032), (11008, 520), (64, 16400), (272, 8200)], ids=str)
+def test_a_token_is_the_same_in_every_batch(gpu_api, size):
+    """Whatever kernel, tile and split of K the number of tokens brings: bit for bit, with every operand of the epilogue, and backward."""
+    K, N = size
+    most = 4096 if N < 2000 else 700
+    w = [t.cuda() for t in ic.drawn_weight(1, K, N)]
+    x = ic.drawn_tokens(2, most, K).cuda()
+    back = [t.cuda() for t in ic.drawn_weight(3, N // 16 * 16, K)]
+    residual_in = torch.randn((most, N // 16 * 16), device="cuda")
+    counts = [T for T in (1, 2, 5, 16, 17, 31, 40, 64, 65, 100, 130, 200, 260, 300, 520, 700, 1031, 2500, 4096) if T <= most]
+    for out_dtype in (F32, BF16):
+        bias, mul, residual = (t.cuda() for t in ec.extras(3, most, N, out_dtype))
+        for k, act in enumerate(ec.ACTS):
+            for use in (1, 2 + k % 2, 4 + k % 2, 7):
+                call = lambda T: gpu_api.forward_int8(  # noqa: E731
+                    x[:T], *w, bias=bias if use & 1 else None, act=act, mul=mul[:T] if use & 2 else None,
+                    residual=residual[:T] if use & 4 else None, keep_z=True, out_dtype=out_dtype)
+                whole = call(most)
+                for T in counts:
+                    for a, b in zip(call(T), whole):
+                        assert torch.equal(a, b[:T]), (out_dtype, act, use, T)
+        r = residual_in.to(out_dtype)
+        whole = gpu_api.backward_int8(x, *back, residual=r, dx_dtype=out_dtype)
+        for T in counts:
+            assert torch.equal(gpu_api.backward_int8(x[:T], *back, residual=r[:T], dx_dtype=out_dtype), whole[:T]), (out_dtype, T)
+
+
+def test_very_many_tokens(gpu_api):
+    """More rows than a launch that brings them to 8 bits takes (2^21)."""
+    T, K, N = 2 ** 21 + 3, 16, 8
+    x = ic.drawn_tokens(5, T, K)
+    codes, scale = ic.drawn_weight(1, K, N)
+    q, s = gpu_api.quantize_tokens(x.cuda())
+    rq, rs = ic.rows8(x.float())
+    same(s, rs), same(q, rq.to(torch.int8))
+    same(gpu_api.forward_int8(x.cuda(), codes.cuda(), scale.cuda()), ic.scaled(ic.products(rq, codes), rs, scale))
+    gu = x.cuda()
+    (q, s), kept = gpu_api.swiglu_forward_int8(gu, 8, keep=True)
+    h, kept2 = gpu_api.swiglu_forward_keep8(gu, 8)
+    for a, b in zip((q, s), gpu_api.quantize_tokens(h)):
+        same(a, b)
+    for k in (kept, kept2):
+        same(gpu_api.restore8(k, 2 * T, 8), ic.restored8(x.view(2 * T, 8)))
+
+
 def test_the_place_of_an_operand(gpu_api):
     """y and z in the place of a bf16 mul or residual of exactly their elements; refused a row further on."""
     for T, d_in, d_out in ((1, 256, 264), (16, 1024, 520), (3, 11008, 264), (100, 2064, 520), (300, 512, 1032), (4090, 144, 6704)):
