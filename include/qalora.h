@@ -286,7 +286,7 @@ int qalora_epilogue_backward(int act, int tokens, int cols, const void* dy, int 
 
 /* A linear in 8-bit integers: a frozen weight (or a merged layer for prompts and serving) and its activations as whole numbers
  * with a scale for each output channel and for each token, products summed exactly in 32 bits.
- *   tokens    v = x (bf16), or v = x factor[i] rounded to fp32;  s[t] = fl32(max_i |v[t,i]| / 127);
+ *   tokens    v = x (bf16), or v = x factor[i] rounded to fp32;  s[t] = fl32(max_i |v[t,i]| fl32(1 / 127));
  *             q[t,i] = the whole number nearest to the quotient v / s (ties to even; of the exact quotient, not of a rounded one).
  *             A row of zeros has s = 0 and codes 0.  A row with an infinity or a NaN in v has s = NaN and codes 0, and so become the
  *             results of that token (no others).

@@ -36,7 +36,7 @@ __device__ __forceinline__ u16x8 swiglu8(const u16x8& g, const u16x8& u) {
   return h;
 }
 
-// ---- one scale a row: s = fl32(top / 127), code = rne(v / s) of the exact quotient -----------------------------------
+// ---- one scale a row: s = fl32(top fl32(1 / 127)), code = rne(v / s) of the exact quotient -----------------------------------
 
 struct RowScale {
   float s;    // as stored: NaN for a row with an infinity or a NaN, then all codes are 0
@@ -48,11 +48,9 @@ struct RowScale {
 __device__ __forceinline__ RowScale row_scale_of(uint32_t top) {
   RowScale r;
   const bool finite = top < 0x7f800000u;
-  // A quotient by a constant: an estimate, its remainder (exact), and one correction give the nearest number (Markstein), but among numbers
-  // so small that the remainder is none any more.
-  const float m = __uint_as_float(top), by127 = 1.0f / 127.0f, estimate = m * by127;
-  float s = __builtin_fmaf(__builtin_fmaf(-estimate, 127.0f, m), by127, estimate);
-  if (top < 0x0d000000u) s = m / 127.0f;  // (below 2^-101)
+  // The largest magnitude times 1 / 127 (which fp32 has to 2^-28), a last place from the quotient at most: what an elementwise division by 127
+  // is on this GPU's tensors, so that scales and codes that a program makes of them are these.
+  const float s = __uint_as_float(top) * (1.0f / 127.0f);
   r.s = finite ? s : __uint_as_float(0x7fc00000u);
   r.up = top < 0x20000000u ? 0x1p64f : 1.0f;  // below 2^-63
   r.by = finite ? s * r.up : 0.0f;

@@ -1,6 +1,6 @@
 // Rows in 8 bits with one scale each: tokens (bf16, as they are, times a factor for each column, or as a SwiGLU's hidden activations)
 // and the channels of a weight.
-//   s = fl32(max |v| / 127),   code = rne(v / s)
+//   s = fl32(max |v| fl32(1 / 127)),   code = rne(v / s)
 // The tokens' kernel reads a row once: a block (or a wavefront, for rows up to 1024 columns) has it whole in registers as bf16 when the
 // largest magnitude is known.  Bound by its bytes, 3 a column (SwiGLU: 5, and 2 more with the kept halves), and nearly as much by its
 // arithmetic, eleven operations a column: 4096 rows of 11008 with factors 30 us, 4.5 TB/s (with a quotient's exactness looked at by 13

@@ -21,7 +21,7 @@ def rows8(v):
     a middle between whole numbers up to 128 by nothing or by at least 2^-26: rounding the 64-bit quotient is rounding the exact one."""
     v = np.asarray(v, dtype=np.float32)
     with np.errstate(all="ignore"):
-        s = np.abs(v).max(1) / np.float32(127)
+        s = np.abs(v).max(1) * np.float32(1 / 127)
         good = np.isfinite(v).all(1)
         d = np.where((s > 0) & good, s, 1).astype(np.float64)
         q = np.clip(np.rint(v.astype(np.float64) / d[:, None]), -127, 127)

@@ -44,7 +44,7 @@ def test_tokens_on_the_border(gpu_api):
     rng = np.random.default_rng(3)
     for top in (1.0, 0.37, 3e-20, 7e-37, 2.1e-38, 5e-42, 8e30):
         top = np.float32(top * (1 + rng.random()))
-        s = top / np.float32(127)
+        s = top * np.float32(1 / 127)
         v = ((rng.integers(-127, 127, cols) + 0.5) * np.float64(s)).astype(np.float32)
         for shift in (-1, 0, 1):
             f = v if shift == 0 else np.nextafter(v, np.float32(shift * np.inf))
@@ -216,7 +216,7 @@ def test_largest_sums(gpu_api):
     x[1] = -1
     codes = torch.full((8, n), 127, dtype=torch.int8, device="cuda")
     scale = torch.ones(8, device="cuda")
-    s = torch.full((2,), np.float32(1) / np.float32(127))
+    s = torch.full((2,), np.float32(1 / 127))
     acc = torch.tensor([[127.0 * 127 * n], [-127.0 * 127 * n]]).expand(2, 8)
     same(gpu_api.forward_int8(x, codes, scale), ic.scaled(acc.double(), s, scale.cpu()))
     back = gpu_api.backward_int8(x, codes.T.contiguous()[:, :8].contiguous().repeat(1, 2), torch.ones(n, device="cuda"))
