@@ -845,7 +845,8 @@ int qalora_quantize_tokens(int tokens, int cols, const void* x, const float* fac
   return launch_tokens8(a, as_stream(stream)) == hipSuccess ? QALORA_OK : QALORA_EHIP;
 }
 
-// Workspace of the products: the codes and scales of the tokens (rows of whole 16 bytes), and the sums of slices of K.
+// Workspace of the products: the codes and scales of the tokens (rows of whole cache lines, so that a step of K is one line of each:
+// 4074 tokens, 2800 -> 8128 150 us, 159 with rows of whole 16 bytes), and the sums of slices of K.
 struct Int8Room {
   size_t q, s, partial, total;
   int ld;
@@ -853,7 +854,7 @@ struct Int8Room {
 static Int8Room int8_room(int tokens, int N, int K) {
   Int8Room p{};
   Carver c;
-  p.ld = round_up(K, 16);
+  p.ld = round_up(K, 128);
   p.s = c.take(sizeof(float) * (size_t)tokens);
   p.q = c.take((size_t)tokens * p.ld);
   p.partial = c.take(int8_partials(tokens, N));
