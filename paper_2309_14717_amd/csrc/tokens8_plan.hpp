@@ -31,7 +31,7 @@ inline Tokens8Plan tokens8_plan(int rows, int cols) {
 // for each (4096 of 4096: 14.7 us, and 17.1 with 1024 blocks).
 inline int tokens8_blocks(const Tokens8Plan& p, int rows, bool plain, bool swiglu) {
   if (plain || rows <= T8_MANY_ROWS) return T8_MOST_ROWS;
-  if (p.lanes <= 256) return swiglu ? 2048 : 3072;
+  if (p.lanes <= 256) return (swiglu ? 512 : 768) * 4;
   if (p.lanes == 512) return p.pieces == 2 ? 1024 : p.pieces == 3 && !swiglu ? 768 : 512;
   return swiglu ? 256 : 512;
 }
