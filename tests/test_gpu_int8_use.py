@@ -177,6 +177,33 @@ def test_products_and_the_kept_captured(gpu_api, shape):
             same(a, c)
 
 
+def test_two_graphs_with_one_workspace(gpu_api):
+    """A forward and a backward, both with K in slices, captured apart on one workspace and replayed in turn, eager calls on it between."""
+    T, d_in, d_out = 40, 4096, 520
+    w = [t.cuda() for t in ic.drawn_weight(1, d_in, d_out)]
+    x, dy = ic.drawn_tokens(2, T, d_in).cuda(), ic.drawn_tokens(3, T, d_out).cuda()
+    n = max(gpu_api.int8_workspace_bytes(T, d_in, d_out, op) for op in (gpu_api.OP_FORWARD, gpu_api.OP_BACKWARD))
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    y, dx = torch.empty((T, d_out), device="cuda"), torch.empty((T, d_in), device="cuda")
+    calls = (lambda: gpu_api.forward_int8(x, *w, ws=ws, y=y), lambda: gpu_api.backward_int8(dy, *w, ws=ws, dx=dx))
+    graphs = []
+    for call in calls:
+        call()
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call()
+    for k in range(4):
+        x.copy_(ic.drawn_tokens(10 + k, T, d_in))
+        dy.copy_(ic.drawn_tokens(20 + k, T, d_out))
+        y.fill_(77), dx.fill_(77), ws.fill_(0x7f)
+        graphs[k % 2].replay()
+        graphs[1 - k % 2].replay()
+        torch.cuda.synchronize()
+        same(y, gpu_api.forward_int8(x, *w)), same(dx, gpu_api.backward_int8(dy, *w))
+        calls[k % 2]()
+
+
 def test_streams_at_once(gpu_api):
     """The same weights on four streams, each call with outputs and workspaces of its own."""
     blocks = [Block(gpu_api, 1024, 1040), Block(gpu_api, 256, 528)]
