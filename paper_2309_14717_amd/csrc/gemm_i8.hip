@@ -295,7 +295,8 @@ __device__ __forceinline__ void gemm_i8_tile(const Int8GemmArgs& p, int8_t* lds,
   for (int b = 0; b < TM; ++b) sc[b] = p.row_scale[min(p.M - 1, m0 + (wm * TM + b) * 16 + fr)];
   const int ch = lane % LPR, col = n0 + wn * CW + 8 * ch, row_in = lane / LPR;
   const bool col_ok = col < p.N && row_in < ROWS_AT_ONCE;  // (N is a multiple of eight)
-  f32x4 bias[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
+  // (without a bias -0 is added, which leaves every sum as it is, one of -0 too: what the other kernels, which add nothing, give)
+  f32x4 bias[2] = {f32x4{-0.0f, -0.0f, -0.0f, -0.0f}, f32x4{-0.0f, -0.0f, -0.0f, -0.0f}};
   if (p.epi.bias && col_ok) {
     bias[0] = reinterpret_cast<const f32x4*>(p.epi.bias + col)[0];
     bias[1] = reinterpret_cast<const f32x4*>(p.epi.bias + col)[1];
