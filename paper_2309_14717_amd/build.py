@@ -39,7 +39,7 @@ FLAGS = [
 NO_SCRATCH = {"gemm_dq.hip": "gemm_dq_kernel", "gemm_dq_192.hip": "gemm_dq_kernel", "gemm_dq_epi.hip": "gemm_dq_kernel", "midt.hip": "midt_kernel", "smallt.hip": "smallt_kernel", "smallt4.hip": "smallt4_kernel", "smallt4_f16.hip": "smallt4_kernel",
               "adapter.hip": ("front_kernel", "front_wide_kernel"), "grads.hip": ("z_kernel", "finish_kernel", "fused_kernel", "du_kernel", "db_kernel", "tail_kernel"),
               "muon.hip": ("muon_start_kernel", "muon_pass_kernel", "muon_alone_kernel"), "epilogue.hip": "epilogue_back_kernel",
-              "tokens8.hip": "tokens8_kernel", "gemm_i8.hip": "gemm_i8_kernel", "stream_i8.hip": "stream_i8_kernel"}
+              "tokens8.hip": "tokens8_kernel", "gemm_i8.hip": ("gemm_i8_kernel", "gemm_i8_mixed_kernel"), "stream_i8.hip": "stream_i8_kernel"}
 
 
 def _as_tuple(v):
@@ -57,6 +57,14 @@ def _check_no_scratch(src: str, remarks: str) -> None:
                 bad.append(name)
     if bad:
         raise RuntimeError(f"{src}: kernels that must not use scratch memory do: {bad}")
+
+
+def _check_names(src: str, remarks: str) -> None:
+    """Fail on a name of NO_SCRATCH that is part of no kernel's: nothing would be looked at for it."""
+    kernels = [line.split("Function Name:")[1].split()[0] for line in remarks.splitlines() if "Function Name:" in line]
+    missing = [n for n in _as_tuple(NO_SCRATCH[src]) if not any(n in k for k in kernels)]
+    if missing:
+        raise RuntimeError(f"{src}: there is no kernel of the name {missing}")
 
 
 def _device_code(obj: str) -> str:
@@ -92,6 +100,7 @@ def _compile(src: str, extra) -> str:
             sys.stderr.write(res.stdout)
             raise subprocess.CalledProcessError(res.returncode, cmd)
         _check_no_scratch(src, res.stdout)
+        _check_names(src, res.stdout)
     else:
         subprocess.check_call(cmd)
     _check_wide_stores(src, _device_code(obj))
