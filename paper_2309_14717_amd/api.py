@@ -61,6 +61,21 @@ class QaloraError(RuntimeError):
         super().__init__(f"{where}: {status_string(status)}")
 
 
+def _c_int(value):
+    """``value``, which ctypes would take modulo 2^32."""
+    if isinstance(value, int) and not -2 ** 31 <= value < 2 ** 31:
+        raise ValueError(f"{value} is no C int")
+    return value
+
+
+class _Int(ctypes.c_int):
+    """A C int in a call."""
+
+    @classmethod
+    def from_param(cls, value):
+        return ctypes.c_int.from_param(_c_int(value))
+
+
 _lib = None
 
 
@@ -74,7 +89,7 @@ def load() -> ctypes.CDLL:
             f"{LIB_PATH} not found: build the HIP library first "
             "(python -m paper_2309_14717_amd.build); there is no fallback path")
     lib = ctypes.CDLL(LIB_PATH)
-    vp, cp, i, sz = ctypes.c_void_p, ctypes.POINTER(Desc), ctypes.c_int, ctypes.c_size_t
+    vp, cp, i, sz = ctypes.c_void_p, ctypes.POINTER(Desc), _Int, ctypes.c_size_t
     lib.qalora_status_string.restype = ctypes.c_char_p
     lib.qalora_status_string.argtypes = [i]
     lib.qalora_check_desc.argtypes = [cp]
@@ -113,8 +128,8 @@ def load() -> ctypes.CDLL:
     lib.qalora_profile_event_destroy.argtypes = [vp]
     lib.qalora_profile_copy.argtypes = [vp, vp, sz, vp]
     lib.qalora_swiglu_forward.argtypes = [vp, vp, vp, sz, vp]
-    lib.qalora_profile_arm_clock.argtypes = [ctypes.c_int, vp]
-    lib.qalora_profile_arm_blocks.argtypes = [ctypes.c_int, vp, ctypes.c_int]
+    lib.qalora_profile_arm_clock.argtypes = [i, vp]
+    lib.qalora_profile_arm_blocks.argtypes = [i, vp, i]
     lib.qalora_profile_mid_blocks.argtypes = [cp, i, ctypes.POINTER(ctypes.c_int)]
     lib.qalora_profile_wall_clock_khz.argtypes = [ctypes.POINTER(ctypes.c_int)]
     lib.qalora_swiglu_backward.argtypes = [vp, vp, vp, vp, vp, sz, vp]
@@ -190,7 +205,7 @@ def status_string(status: int) -> str:
 
 
 def make_desc(d_in, d_out, bits=4, group=32, rank=0, s=0.0) -> Desc:
-    return Desc(int(d_in), int(d_out), int(bits), int(group), int(rank), float(s))
+    return Desc(*(_c_int(int(v)) for v in (d_in, d_out, bits, group, rank)), float(s))
 
 
 def check_desc(desc: Desc) -> int:
