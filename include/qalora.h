@@ -337,7 +337,8 @@ size_t qalora_kept8_bytes(int tokens, int cols);
 int qalora_keep8(int tokens, int cols, const void* x, void* kept, void* stream);         /* x bf16 */
 int qalora_restore8(int tokens, int cols, const void* kept, void* x, void* stream);      /* x bf16 */
 /* SwiGLU on gu = [gate | up], bf16 [tokens, 2 cols], with what follows it in the same pass; each output may be NULL, but not all:
- *   h     silu(gate) up, bf16 [tokens, cols]: in fp32 to (8 + 4 |gate|) 2^-24 of itself, rounded once; the same whatever else is asked for
+ *   h     silu(gate) up, bf16 [tokens, cols]: in fp32 to (8 + 4 |gate|) 2^-24 of itself, rounded once; the same whatever else is asked for.
+ *         (For gates below -87.33, where |silu(gate)| is below 2^-119, it is zero.)
  *   q, s  its codes and scales, as qalora_quantize_tokens makes them of the bf16 h: the down projection's input (together; cols at most
  *         QALORA_INT8_MAX_SIDE, QALORA_EUNSUPPORTED otherwise)
  *   kept  gate and up for the backward: what qalora_keep8 makes of gu as [2 tokens, cols], qalora_kept8_bytes(2 tokens, cols) bytes

@@ -87,3 +87,24 @@ def test_a_large_batch_is_its_parts(gpu_api, size):
                 for at in some:
                     for part, all_rows in zip(call(at), whole):
                         alike(part, all_rows[at])
+
+
+@pytest.mark.parametrize("up", [1.0, -3.0, 1e30])
+def test_hidden_activations_of_very_negative_gates(gpu_api, up):
+    """As documented: (8 + 4 |gate|) 2^-24 of themselves, and half a step of bf16, down to gates of -87.33; zero below, where a silu
+    is less than 2^-119.  (Half a step of a subnormal bf16 number is 2^-134.)"""
+    gate = torch.cat([torch.arange(-110, -79.75, 0.25), torch.arange(-87.5, -86.5, 2.0 ** -4)]).to(BF16)
+    C = gate.numel() // 8 * 8
+    gate = gate[:C]
+    gu = torch.cat([gate, torch.full((C,), up, dtype=BF16)])[None].cuda()
+    h, _ = gpu_api.swiglu_forward_keep8(gu, C)
+    h2 = torch.empty_like(h)
+    gpu_api.swiglu_forward_int8(gu, C, h=h2)
+    alike(h2, h)
+    g = gate.double()
+    ref = g * torch.sigmoid(g) * float(torch.tensor(up).to(BF16))
+    tol = (8 + 4 * g.abs()) * 2.0 ** -24 * ref.abs()
+    off = (h[0].cpu().double() - ref).abs()
+    near = off <= tol + 2.0 ** -8 * (ref.abs() + tol) + 2.0 ** -134
+    assert near[g > -87.33].all()
+    assert (h[0].cpu()[g < -87.34] == 0).all() and (ref.abs()[g < -87.34] < 2.0 ** -119 * abs(up) * (1 + 2.0 ** -8)).all()
