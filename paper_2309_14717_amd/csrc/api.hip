@@ -887,7 +887,7 @@ int qalora_forward_int8(int tokens, int d_in, int d_out, const void* x, const fl
       any_overlap({y, n * (y_dtype == QALORA_BF16 ? 2 : 4)}, {weights, scales, x_scales}) ||
       any_overlap({e.z, 2 * n}, {weights, scales, x_scales}))
     return QALORA_EINVAL;
-  if (!x_scale && stream8_takes(tokens, d_in)) {
+  if (!x_scale && stream8_takes(tokens, d_in, d_out)) {
     StreamI8Args a{};
     a.x = static_cast<const uint16_t*>(x);
     a.codes = codes;
