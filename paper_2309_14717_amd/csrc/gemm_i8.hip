@@ -3,8 +3,8 @@
 //   backward  dx[t, i] = s[t] sum_j q[t, j] w8[j, i]            K = d_out (the channels' scales are in q)
 // and the epilogue on that.  One copy of the weight's codes, [d_out, d_in], serves both directions: the forward's operands lie along K in
 // it, the backward's are turned by transposing LDS reads.
-// Large products are bound by the matrix instructions and the chip's power: 4096 tokens, K = 11008, 4096 columns, either direction 147 us,
-// 2500 TOP/s.  A step of K is 128, whole cache lines of every row (64: 216 us for 4096 x 11008 x 4096 that take 180); the backward's reads
+// Large products are bound by the matrix instructions and the chip's power: 4096 tokens, K = 11008, 4096 columns, either direction 152 us
+// behind a pause, 2430 TOP/s, and 164 one after the other.  A step of K is 128, whole cache lines of every row (64: 216 us for 4096 x 11008 x 4096 that take 180); the backward's reads
 // wait in a block of their own (by the builtin, before which all loads on their way are waited for: 183 us).
 #include <atomic>
 #include <type_traits>

@@ -1,7 +1,7 @@
 // Activations kept in 8 bits for the backward: 32 neighbouring columns of a row share the exponent of their largest magnitude, codes
 // are whole multiples of 2^(E - 133).  What comes back are bf16 numbers.
 // Elementwise passes bound by their bytes: a lane has eight columns, four lanes a group.  4096 x 11008: SwiGLU 68 us each way (5.3 TB/s);
-// 1531 x 13824 kept alone 13.5 us (4.7 TB/s).
+// 1531 x 13824 kept alone 12.6 us (5.1 TB/s), restored 12.1.
 #include "int8.hpp"
 #include "kernels.hpp"
 #include "swiglu.hpp"

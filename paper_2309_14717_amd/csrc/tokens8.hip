@@ -1,11 +1,11 @@
 // Rows in 8 bits with one scale each: tokens (bf16, as they are, times a factor for each column, or as a SwiGLU's hidden activations)
 // and the channels of a weight.
 //   s = fl32(max |v| fl32(1 / 127)),   code = rne(v / s)
-// The tokens' kernel reads a row once: a block (or a wavefront, for rows up to 1024 columns) has it whole in registers as bf16 when the
-// largest magnitude is known.  Bound by its bytes, 3 a column (SwiGLU: 5, and 2 more with the kept halves), and nearly as much by its
-// arithmetic, eleven operations a column: 4096 rows of 11008 with factors 30 us, 4.5 TB/s (with a quotient's exactness looked at by 13
-// operations 36 us), 4096 plain ones of 4096 14.2 us, 1531 rows of 13824 hidden activations 25 us; without the codes' arithmetic
-// the last two take 11.3 and 22.
+// The tokens' kernel reads a row once, up to 65536 columns (hidden activations: 32768; longer rows twice): a block (or a wavefront, for rows
+// up to 1024 columns) has it whole in registers as bf16 when the largest magnitude is known.  Bound by its bytes, 3 a column (SwiGLU: 5,
+// and 2 more with the kept halves), and a good part of them by its arithmetic, eleven operations a column: 4096 rows of 11008 with
+// factors 26.6 us, 5.1 TB/s, 4096 plain ones of 4096 12.5 us, 1531 rows of 13824 hidden activations 22 us (kept too: 33.5); without the
+// codes' arithmetic 24.6, 10.0 and 20.
 #include "int8.hpp"
 #include "kernels.hpp"
 #include "tokens8_plan.hpp"
@@ -186,7 +186,8 @@ hipError_t launch_tokens8(const Tokens8Args& args, hipStream_t st) {
 }
 
 // ---- a weight's channels -------------------------------------------------------------------------------------------------
-// W [d_in, d_out] fp32, or alpha code + beta (one rounding) of a quantized layer, to codes [d_out, d_in].  Done once for a model: the
+// W [d_in, d_out] fp32, or alpha code + beta (one rounding) of a quantized layer, to codes [d_out, d_in].  Done once for a model (4096 x 11008 115 us, 8192 x
+// 22016 440; of INT4 layers 130 and 420: W, or the packed codes, are read twice, by a lane a channel): the
 // channels' largest magnitudes (by atomic maxima of their bits, whose order does not matter), then the codes, then the scales.
 
 template <int NBITS>  // 0: W

@@ -13,7 +13,7 @@ struct Tokens8Plan {
   int rows;    // of a block at once
 };
 // Many rows: as few threads a row as hold it in four pieces each, so that a compute unit has many rows on their way (4096 rows of 11008 with
-// factors: 29.6 us with 512 threads of three pieces, 33.6 with 256 of six, 37.8 with 1024 of two); few rows: as many threads as there are.
+// factors: 26.6 us with 512 threads of three pieces, 30.6 with 256 of six, 35.3 with 1024 of two); few rows: as many threads as there are.
 constexpr int T8_MANY_ROWS = 512;
 inline Tokens8Plan tokens8_plan(int rows, int cols) {
   const int eights = (cols + 7) / 8;
@@ -26,9 +26,9 @@ inline Tokens8Plan tokens8_plan(int rows, int cols) {
   return p;
 }
 // Blocks of a launch at most: where a row's loads wait for more than its bytes (factors, hidden activations), as many as the chip has room for
-// at once, each with every so manyth row, the next on its way meanwhile (4096 rows of 11008 with factors: 768 blocks 29.6 us, a block
-// a row 33.2; of 13824 512 blocks 39.8, 768 47.6; 1531 of 22016 hidden activations: 256 blocks 40.2, 512 44.6).  Plain rows: a block
-// for each (4096 of 4096: 14.7 us, and 17.1 with 1024 blocks).
+// at once, each with every so manyth row, the next on its way meanwhile (4096 rows of 11008 with factors: 768 blocks 26.6 us, a block
+// a row 31.1; of 13824 512 blocks 34.9, 768 42.2; 1531 of 22016 hidden activations: 256 blocks 36.1, 512 41.3).  Plain rows: a block
+// for each (4096 of 4096: 12.5 us, and 14.6 with 1024 blocks).
 inline int tokens8_blocks(const Tokens8Plan& p, int rows, bool plain, bool swiglu) {
   if (plain || rows <= T8_MANY_ROWS) return T8_MOST_ROWS;
   if (p.lanes <= 256) return (swiglu ? 512 : 768) * 4;
