@@ -25,13 +25,13 @@ def test_room(takes):
         assert not takes(T, K, N) or (T <= 16 and T * K <= 16384)
 
 
-@pytest.mark.parametrize("size", [(1, 16, 8), (16, 1024, 1024), (16, 1024, 4096), (8, 1024, 8192), (4, 4096, 4096), (1, 4096, 11008), (2, 8192, 8192),
+@pytest.mark.parametrize("size", [(1, 16, 8), (16, 1024, 1024), (16, 1024, 4096), (8, 1024, 8192), (16, 1024, 8192), (8, 1024, 12288), (1, 1024, 13824), (4, 4096, 4096), (1, 4096, 11008), (2, 8192, 8192),
                                   (1, 8192, 22016), (1, 11008, 4096), (1, 16384, 131072)], ids=str)
 def test_one_launch(takes, size):
     assert takes(*size)
 
 
-@pytest.mark.parametrize("size", [(17, 16, 8), (16, 1040, 8), (16, 1024, 8192), (16, 1024, 22016), (8, 2048, 22016), (16, 256, 131072),
+@pytest.mark.parametrize("size", [(17, 16, 8), (16, 1040, 8), (16, 1024, 9216), (16, 1024, 22016), (8, 2048, 22016), (16, 256, 131072),
                                   (1, 1024, 65536), (2, 8192, 22016), (1, 16400, 8)], ids=str)
 def test_two_launches(takes, size):
     assert not takes(*size)
